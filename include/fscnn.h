@@ -442,6 +442,66 @@ fscnn_status_t fscnn_sparse_tensor_transpose(const int *rowptr_dev, const unsign
  * Host-only. */
 long long fscnn_sparse_transpose_workspace(long long new_rows, long long nnz);
 
+/* ------------------------------------------------------------------ weights in 4 bits
+ * The fully connected layers behind the convolutions, and the projections of language models: K rows of C weights, held as
+ *   w[k][c] = scale[k][g] * (code[k][c] - zero[k][g]),   g = c / group,   code in 0..15, zero in 0..15 (8 where none is given),
+ * group 32, 64 or 128, with ceil(C/group) scales a row (the last group may be short).  Scales are fp16 or bf16 and kept as they are. */
+typedef int fscnn_dtype_t;
+enum { FSCNN_F32 = 0, FSCNN_F16 = 1, FSCNN_BF16 = 2, FSCNN_I8 = 3 };
+typedef struct fscnn_q4 fscnn_q4_t;
+
+/* 4-bit weights of a dense K x C matrix w_dev of type w_type (F32, F16, BF16; rows ldw >= C elements apart, aligned to the type).
+ * zeros == 0: scale = max|w| / 7 of the group, zero point 8; otherwise scale = (hi - lo) / 15, zero = rint(-lo / scale) with
+ * lo = min(0, w), hi = max(0, w).  The scale is rounded to fp16 for fp16 weights and to bf16 otherwise, and
+ * code = min(max(rint(w / scale) + zero, 0), 15) with the rounded scale; a group of zeros has scale 0, one with an infinite weight or a NaN
+ * scale NaN.  Runs on `stream` and waits until the handle is written: then w_dev may go and any stream use the handle.  A capturing
+ * stream is refused (FSCNN_ERR_UNSUPPORTED).  C up to 2^20. */
+fscnn_status_t fscnn_q4_compress(const void *w_dev, fscnn_dtype_t w_type, int K, int C, long long ldw, int group, int zeros,
+                                 void *stream, fscnn_q4_t **out);
+
+/* The same from codes that exist: codes_dev K x ceil(C/2) bytes, column 2 i in the low and 2 i + 1 in the high four bits of byte i (the
+ * high bits of an odd row's last byte are ignored); scales_dev K x ceil(C/group) of scale_type (F16, BF16); zeros_dev
+ * K x ceil(C/group) bytes of 0..15, or NULL for 8.  FSCNN_ERR_UNSUPPORTED if a zero point is above 15.  Waits as above. */
+fscnn_status_t fscnn_q4_import(const unsigned char *codes_dev, const void *scales_dev, fscnn_dtype_t scale_type,
+                               const unsigned char *zeros_dev, int K, int C, int group, void *stream, fscnn_q4_t **out);
+
+/* Any output pointer may be NULL; *zeros: whether the handle has zero points of its own. */
+fscnn_status_t fscnn_q4_info(const fscnn_q4_t *q, int *K, int *C, int *group, int *zeros, fscnn_dtype_t *scale_type);
+
+/* Codes, scales and zero points (NULL, or 8 where the handle has none of its own) as fscnn_q4_import takes them, copied to HOST buffers; the high bits of an odd row's
+ * last byte are 0.  Synchronous. */
+fscnn_status_t fscnn_q4_export(const fscnn_q4_t *q, unsigned char *codes_host, void *scales_host, unsigned char *zeros_host);
+fscnn_status_t fscnn_q4_destroy(fscnn_q4_t *q);
+
+/* y[m][k] = act(sum over c of w[k][c] * x[m][c] + bias_dev[k]),  act(a) = a > 0 ? a : negative_slope * a.
+ * x_dev: M rows of C elements of x_type, rows ldx >= C elements apart; y_dev: M rows of K elements of y_type (F32, F16, BF16), rows
+ * ldy >= K elements apart, what lies between them is left as it is; both aligned to their type (16-byte aligned rows are read faster).
+ * bias_dev: K floats or NULL.  negative_slope in [0, 1]: 1 no activation, 0 ReLU, between them LeakyReLU; else FSCNN_ERR_SHAPE.
+ * x_type F32, F16, BF16: x_scale_dev NULL; products are formed with the codes as they are, sums are held in fp32 and every group's is
+ * multiplied by its scale in fp32; y is rounded once.  (F32: x enters as three bfloat16 parts, their sum within 2^-24 of it.)
+ * x_type I8: x[m][c] stands for x_dev[m][c] * x_scale, x_scale_dev M x x_scale_cols floats, one for the row (x_scale_cols 1) or one for
+ * each group of the weights (ceil(C/group)); a group's sum is exact in 32-bit integers.
+ * An x that is not finite meets every weight of its row, zeros among them; other rows are not touched by it.  M == 0 is no work (pointers
+ * to x and y may be NULL then).  y must not overlap x.  Allocates nothing, does not synchronise, needs no scratch; results are run-to-run
+ * identical.  Calls on any streams may share a handle.  FSCNN_ERR_MISMATCH if C differs from the handle's, or the current device.
+ * M < 2^31 with M * ldx and M * ldy below 2^62. */
+fscnn_status_t fscnn_linear_q4(const fscnn_q4_t *q, const void *x_dev, fscnn_dtype_t x_type, long long ldx, const float *x_scale_dev,
+                               int x_scale_cols, int M, int C, const float *bias_dev, float negative_slope, void *y_dev,
+                               fscnn_dtype_t y_type, long long ldy, void *stream);
+
+/* Root-mean-square norm of M rows of D elements, with the residual's addition before it and an 8-bit output behind it:
+ *   h = x (+ residual),   y = h / sqrt(mean over the row of h^2 + eps) * weight,
+ * sums in fp32, h as it is before it is rounded.  x_dev, residual_dev (NULL: none) and residual_out_dev (receives h; NULL: not wanted; only
+ * with a residual) are of type x_type (F32, F16, BF16), weight_dev (NULL: ones) of weight_type, rows ldx, ldr, ldo, ldy >= D elements apart.
+ * y_type F32, F16, BF16: scale_dev NULL, group 0.  y_type I8: y_dev receives rint(y / scale) in -127..127 with
+ * scale = max|y| / 127 over the row (group 0, scale_dev M floats) or over each group of 32, 64 or 128 elements (scale_dev
+ * M x ceil(D/group) floats) -- what fscnn_linear_q4 takes; where all are zero, or one is not finite, the codes are 0 and the scale is max|y| / 127.
+ * In place: y_dev, if y has x's type, and residual_out_dev may each be x_dev or residual_dev with the same row distance; no other overlap.
+ * D up to 65536.  M == 0 is no work.  eps >= 0.  Allocates nothing, does not synchronise. */
+fscnn_status_t fscnn_rms_norm(const void *x_dev, fscnn_dtype_t x_type, long long ldx, const void *residual_dev, long long ldr,
+                              void *residual_out_dev, long long ldo, const void *weight_dev, fscnn_dtype_t weight_type, int M, int D,
+                              float eps, void *y_dev, fscnn_dtype_t y_type, long long ldy, float *scale_dev, int group, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -22,7 +22,8 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 OBJDIR = os.path.join(ROOT, "_build")
 LIB = os.path.join(HERE, "libfscnn.so")
-SOURCES = ["api.hip", "compress.hip", "conv_sf.hip", "conv_si.hip", "contract.hip", "contract_split.hip", "pointwise.hip", "transpose.hip"]
+SOURCES = ["api.hip", "compress.hip", "conv_sf.hip", "conv_si.hip", "contract.hip", "contract_split.hip", "pointwise.hip", "transpose.hip",
+           "q4.hip", "q4_linear.hip", "rms_norm.hip"]
 PROBE_LIB = os.path.join(HERE, "libfscnn_bench_probe.so")
 PROBE_SRC = os.path.join(CSRC, "bench_probe.hip")
 CALL_LIB = os.path.join(HERE, "_fscnn_call.so")
@@ -79,7 +80,7 @@ def build_host_sanitized(verbose=True):
 
 def build(force=False, extra_flags=(), verbose=True):
     os.makedirs(OBJDIR, exist_ok=True)
-    headers = [os.path.join(CSRC, "internal.h"), os.path.join(CSRC, "arrival.h"), os.path.join(CSRC, "host_word.h"), os.path.join(CSRC, "lds_dma.h"),
+    headers = [os.path.join(CSRC, "internal.h"), os.path.join(CSRC, "arrival.h"), os.path.join(CSRC, "host_word.h"), os.path.join(CSRC, "lds_dma.h"), os.path.join(CSRC, "lowbits.h"),
                os.path.join(ROOT, "include", "fscnn.h"),
                os.path.abspath(__file__)]
     jobs, objs = [], []

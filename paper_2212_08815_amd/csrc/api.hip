@@ -57,6 +57,12 @@ fscnn_status_t have_device(int *dev)
 bool live(const fscnn_filter_t *f) { return f && f->magic == kFilterMagic; }
 bool live(const fscnn_input_t *i) { return i && i->magic == kInputMagic; }
 bool live(const fscnn_dense_t *d) { return d && d->magic == kDenseMagic; }
+bool live(const fscnn_q4_t *q) { return q && q->magic == kQ4Magic; }
+
+// Bytes of an element of a type that tensors may have; 0: not one
+int type_bytes(fscnn_dtype_t t) { return t == FSCNN_F32 ? 4 : t == FSCNN_F16 || t == FSCNN_BF16 ? 2 : t == FSCNN_I8 ? 1 : 0; }
+bool float_type(fscnn_dtype_t t) { return type_bytes(t) >= 2; }
+bool misaligned(const void *p, fscnn_dtype_t t) { return ((uintptr_t)p & (type_bytes(t) - 1)) != 0; }
 
 // Share of a bank's entries that are stored (1 exactly for a bank without zeros).
 double density(const fscnn_filter_t *f) { return (double)f->nnz / ((double)f->K * f->C * f->R * f->S); }
@@ -1630,6 +1636,191 @@ fscnn_status_t fscnn_maxpool2x2(const float *x_dev, int N, int C, int H, int W, 
                                 void *stream)
 {
     return fscnn_maxpool2x2_ex(x_dev, N, C, H, W, y_dev, FSCNN_LAYOUT_NCHW, stream);
+}
+
+// A handle for K x C weights, its buffers allocated; `type` of the scales
+static fscnn_status_t q4_new(int K, int C, int group, int zeros, int type, hipStream_t st, fscnn_q4_t **out)
+{
+    if (K <= 0 || C <= 0) return FSCNN_ERR_SHAPE;
+    if (group != 32 && group != 64 && group != 128) return FSCNN_ERR_UNSUPPORTED;
+    if (C > 1 << 20) return FSCNN_ERR_UNSUPPORTED;
+    int dev;
+    fscnn_status_t s = have_device(&dev);
+    if (s != FSCNN_OK) return s;
+    if (capturing(st)) return FSCNN_ERR_UNSUPPORTED;
+    fscnn_q4_t *q = new (std::nothrow) fscnn_q4();
+    if (!q) return FSCNN_ERR_ALLOC;
+    q->magic = kQ4Magic;
+    q->device = dev;
+    q->K = K; q->C = C; q->group = group;
+    q->zeros = zeros != 0;
+    q->scale_type = type;
+    const size_t codes = q4_code_bytes(K, C);
+    // (behind the scales: the flag of launch_q4_import)
+    const hipError_t e = device_alloc(reinterpret_cast<void **>(&q->codes), codes + q4_scale_bytes(K, C, group) + 256);
+    if (e != hipSuccess) {
+        (void)hipGetLastError();
+        delete q;
+        return e == hipErrorOutOfMemory ? FSCNN_ERR_ALLOC : FSCNN_ERR_DEVICE;
+    }
+    q->scales = reinterpret_cast<uint32_t *>(reinterpret_cast<char *>(q->codes) + codes);
+    *out = q;
+    return FSCNN_OK;
+}
+
+static void q4_delete(fscnn_q4_t *q)
+{
+    q->magic = 0;
+    (void)hipFree(q->codes);   // with the scales
+    delete q;
+}
+
+fscnn_status_t fscnn_q4_compress(const void *w_dev, fscnn_dtype_t w_type, int K, int C, long long ldw, int group, int zeros,
+                                 void *stream, fscnn_q4_t **out)
+{
+    if (!w_dev || !out) return FSCNN_ERR_NULL;
+    if (!float_type(w_type)) return FSCNN_ERR_UNSUPPORTED;
+    if (K > 0 && C > 0 && (ldw < C || ldw > (1LL << 31))) return FSCNN_ERR_SHAPE;
+    if (misaligned(w_dev, w_type)) return FSCNN_ERR_UNSUPPORTED;
+    fscnn_q4_t *q;
+    const fscnn_status_t s = q4_new(K, C, group, zeros, w_type == FSCNN_F16 ? FSCNN_F16 : FSCNN_BF16, (hipStream_t)stream, &q);
+    if (s != FSCNN_OK) return s;
+    hipError_t e = launch_q4_compress(q, w_dev, w_type, ldw, (hipStream_t)stream);
+    if (e == hipSuccess) e = hipStreamSynchronize((hipStream_t)stream);
+    if (e != hipSuccess) {
+        (void)hipGetLastError();
+        q4_delete(q);
+        return FSCNN_ERR_DEVICE;
+    }
+    *out = q;
+    return FSCNN_OK;
+}
+
+fscnn_status_t fscnn_q4_import(const unsigned char *codes_dev, const void *scales_dev, fscnn_dtype_t scale_type,
+                               const unsigned char *zeros_dev, int K, int C, int group, void *stream, fscnn_q4_t **out)
+{
+    if (!codes_dev || !scales_dev || !out) return FSCNN_ERR_NULL;
+    if (scale_type != FSCNN_F16 && scale_type != FSCNN_BF16) return FSCNN_ERR_UNSUPPORTED;
+    if (misaligned(scales_dev, scale_type)) return FSCNN_ERR_UNSUPPORTED;
+    fscnn_q4_t *q;
+    const fscnn_status_t s = q4_new(K, C, group, zeros_dev != nullptr, scale_type, (hipStream_t)stream, &q);
+    if (s != FSCNN_OK) return s;
+    int *flag = reinterpret_cast<int *>(reinterpret_cast<char *>(q->scales) + q4_scale_bytes(K, C, group)), bad = 0;
+    hipError_t e = launch_q4_import(q, codes_dev, scales_dev, zeros_dev, flag, (hipStream_t)stream);
+    if (e == hipSuccess) e = hipStreamSynchronize((hipStream_t)stream);
+    if (e == hipSuccess && zeros_dev) e = hipMemcpy(&bad, flag, sizeof(int), hipMemcpyDeviceToHost);
+    if (e != hipSuccess || bad) {
+        (void)hipGetLastError();
+        q4_delete(q);
+        return e != hipSuccess ? FSCNN_ERR_DEVICE : FSCNN_ERR_UNSUPPORTED;
+    }
+    *out = q;
+    return FSCNN_OK;
+}
+
+fscnn_status_t fscnn_q4_info(const fscnn_q4_t *q, int *K, int *C, int *group, int *zeros, fscnn_dtype_t *scale_type)
+{
+    if (!q) return FSCNN_ERR_NULL;
+    if (!live(q)) return FSCNN_ERR_HANDLE;
+    if (K) *K = q->K;
+    if (C) *C = q->C;
+    if (group) *group = q->group;
+    if (zeros) *zeros = q->zeros;
+    if (scale_type) *scale_type = q->scale_type;
+    return FSCNN_OK;
+}
+
+fscnn_status_t fscnn_q4_export(const fscnn_q4_t *q, unsigned char *codes_host, void *scales_host, unsigned char *zeros_host)
+{
+    if (!q || !codes_host || !scales_host) return FSCNN_ERR_NULL;
+    if (!live(q)) return FSCNN_ERR_HANDLE;
+    int dev;
+    fscnn_status_t s = have_device(&dev);
+    if (s != FSCNN_OK) return s;
+    if (dev != q->device) return FSCNN_ERR_MISMATCH;
+    const size_t nc = (size_t)q->K * (((size_t)q->C + 1) / 2), ns = (size_t)q->K * (((size_t)q->C + q->group - 1) / q->group);
+    const size_t at = (nc + 255) / 256 * 256;
+    char *buf = nullptr;
+    hipError_t e = device_alloc(reinterpret_cast<void **>(&buf), at + 3 * ns);
+    if (e != hipSuccess) {
+        (void)hipGetLastError();
+        return e == hipErrorOutOfMemory ? FSCNN_ERR_ALLOC : FSCNN_ERR_DEVICE;
+    }
+    unsigned char *codes = reinterpret_cast<unsigned char *>(buf), *zeros = codes + at + 2 * ns;
+    e = launch_q4_export(q, codes, buf + at, zeros, nullptr);
+    if (e == hipSuccess) e = hipMemcpy(codes_host, codes, nc, hipMemcpyDeviceToHost);
+    if (e == hipSuccess) e = hipMemcpy(scales_host, buf + at, 2 * ns, hipMemcpyDeviceToHost);
+    if (e == hipSuccess && zeros_host) e = hipMemcpy(zeros_host, zeros, ns, hipMemcpyDeviceToHost);
+    (void)hipFree(buf);
+    FSCNN_HIP(e);
+    return FSCNN_OK;
+}
+
+fscnn_status_t fscnn_q4_destroy(fscnn_q4_t *q)
+{
+    if (!q) return FSCNN_ERR_NULL;
+    if (!live(q)) return FSCNN_ERR_HANDLE;
+    q4_delete(q);
+    return FSCNN_OK;
+}
+
+fscnn_status_t fscnn_linear_q4(const fscnn_q4_t *q, const void *x_dev, fscnn_dtype_t x_type, long long ldx, const float *x_scale_dev,
+                               int x_scale_cols, int M, int C, const float *bias_dev, float negative_slope, void *y_dev,
+                               fscnn_dtype_t y_type, long long ldy, void *stream)
+{
+    if (!q || (M != 0 && (!x_dev || !y_dev))) return FSCNN_ERR_NULL;
+    if (!live(q)) return FSCNN_ERR_HANDLE;
+    if (M < 0 || C <= 0 || !(negative_slope >= 0.0f && negative_slope <= 1.0f)) return FSCNN_ERR_SHAPE;
+    if (C != q->C) return FSCNN_ERR_MISMATCH;
+    if (!type_bytes(x_type) || !float_type(y_type)) return FSCNN_ERR_UNSUPPORTED;
+    if (M == 0) return FSCNN_OK;
+    if (ldx < C || ldy < q->K || ldx > (1LL << 62) / M || ldy > (1LL << 62) / M) return FSCNN_ERR_SHAPE;
+    if (x_type == FSCNN_I8) {
+        if (!x_scale_dev) return FSCNN_ERR_NULL;
+        if (x_scale_cols != 1 && x_scale_cols != (C + q->group - 1) / q->group) return FSCNN_ERR_MISMATCH;
+        if (misaligned(x_scale_dev, FSCNN_F32)) return FSCNN_ERR_UNSUPPORTED;
+    } else if (x_scale_dev) {
+        return FSCNN_ERR_UNSUPPORTED;
+    }
+    if (misaligned(x_dev, x_type) || misaligned(y_dev, y_type) || misaligned(bias_dev, FSCNN_F32) || x_dev == y_dev) return FSCNN_ERR_UNSUPPORTED;
+    int dev;
+    const fscnn_status_t s = have_device(&dev);
+    if (s != FSCNN_OK) return s;
+    if (dev != q->device) return FSCNN_ERR_MISMATCH;
+    FSCNN_HIP(launch_linear_q4(q, x_dev, x_type, ldx, x_scale_dev, x_scale_cols, M, bias_dev, negative_slope == 1.0f ? 0 : act_code(negative_slope),
+                               y_dev, y_type, ldy, (hipStream_t)stream));
+    return FSCNN_OK;
+}
+
+fscnn_status_t fscnn_rms_norm(const void *x_dev, fscnn_dtype_t x_type, long long ldx, const void *residual_dev, long long ldr,
+                              void *residual_out_dev, long long ldo, const void *weight_dev, fscnn_dtype_t weight_type, int M, int D,
+                              float eps, void *y_dev, fscnn_dtype_t y_type, long long ldy, float *scale_dev, int group, void *stream)
+{
+    if (M < 0 || D <= 0 || !(eps >= 0.0f)) return FSCNN_ERR_SHAPE;
+    if (M != 0 && (!x_dev || !y_dev || (y_type == FSCNN_I8 && !scale_dev))) return FSCNN_ERR_NULL;
+    if (!float_type(x_type) || !type_bytes(y_type) || (weight_dev && !float_type(weight_type)) || D > kNormMaxD) return FSCNN_ERR_UNSUPPORTED;
+    if (y_type == FSCNN_I8 ? group != 0 && group != 32 && group != 64 && group != 128 : group != 0 || scale_dev) return FSCNN_ERR_UNSUPPORTED;
+    if (residual_out_dev && !residual_dev) return FSCNN_ERR_UNSUPPORTED;
+    if (M == 0) return FSCNN_OK;
+    const long long most = (1LL << 62) / M;
+    if (ldx < D || ldy < D || ldx > most || ldy > most) return FSCNN_ERR_SHAPE;
+    if (residual_dev && (ldr < D || ldr > most)) return FSCNN_ERR_SHAPE;
+    if (residual_out_dev && (ldo < D || ldo > most)) return FSCNN_ERR_SHAPE;
+    if (misaligned(x_dev, x_type) || misaligned(residual_dev, x_type) || misaligned(residual_out_dev, x_type) || misaligned(y_dev, y_type) ||
+        (weight_dev && misaligned(weight_dev, weight_type)) || misaligned(scale_dev, FSCNN_F32))
+        return FSCNN_ERR_UNSUPPORTED;
+    // (a row is read whole before it is written, rows in any order: in place only element for element)
+    auto clash = [&](const void *out, long long ld, bool same_type) {
+        return (out == x_dev && (!same_type || (ld != ldx && M > 1))) || (residual_dev && out == residual_dev && (!same_type || (ld != ldr && M > 1)));
+    };
+    if (clash(y_dev, ldy, y_type == x_type) || (residual_out_dev && (clash(residual_out_dev, ldo, true) || residual_out_dev == y_dev)))
+        return FSCNN_ERR_UNSUPPORTED;
+    int dev;
+    const fscnn_status_t s = have_device(&dev);
+    if (s != FSCNN_OK) return s;
+    FSCNN_HIP(launch_rms_norm(x_dev, x_type, ldx, residual_dev, ldr, residual_out_dev, ldo, weight_dev, weight_type, M, D, eps, y_dev, y_type,
+                              ldy, scale_dev, group, (hipStream_t)stream));
+    return FSCNN_OK;
 }
 
 }  // extern "C"

@@ -15,6 +15,7 @@ namespace fscnn {
 constexpr uint64_t kFilterMagic = 0x4653434e4e464c54ull;  // "FSCNNFLT"
 constexpr uint64_t kInputMagic = 0x4653434e4e494e50ull;   // "FSCNNINP"
 constexpr uint64_t kDenseMagic = 0x4653434e4e44454eull;   // "FSCNNDEN"
+constexpr uint64_t kQ4Magic = 0x4653434e4e513442ull;      // "FSCNNQ4B"
 
 // One nonzero as the convolution kernel streams it: the byte offset of the tap
 // (c mod CC, r, s) inside the LDS input tile, and the weight (the paper's node
@@ -191,7 +192,44 @@ struct fscnn_dense {
     int *flag;       // 3x3: non-zero if the bank holds an Inf or NaN
 };
 
+// Weights in 4 bits, K rows of C, laid out for the matrix cores' operands (q4.hip): tiles of 16 rows, blocks of 128 columns.
+struct fscnn_q4 {
+    uint64_t magic;
+    int device;
+    int K, C, group;
+    int zeros;             // zero points of their own (else 8)
+    int scale_type;        // of the scales as they were given: FSCNN_F16 or FSCNN_BF16
+    uint32_t *codes;       // device [tiles][blocks][64 lanes][4]; owns the allocation
+    uint32_t *scales;      // device [tiles][blocks * 128 / group][16 rows], behind the codes
+};
+
 namespace fscnn {
+
+// ---- q4.hip: 4-bit weights.  Word s of lane l of a block holds the eight codes of row l % 16 whose columns in the block are
+// 32 s + 8 (l / 16) + j, j = 0..7: code j in nibble 2 j for j < 4, else in nibble 2 (j - 4) + 1.  (A step of 32 columns of the matrix
+// cores' 16-row operand; the nibbles of a parity, masked out, are four codes in bytes.)  Columns past C hold the zero point, rows past K
+// zeros with a scale of zero.  A scale is the word of its value as a float, which 16-bit types leave at least 13 low bits of: the zero
+// point is in the low four.
+constexpr int kQ4Block = 128;
+inline long long q4_tiles(int K) { return ((long long)K + 15) / 16; }
+inline long long q4_blocks(int C) { return ((long long)C + kQ4Block - 1) / kQ4Block; }
+inline size_t q4_code_bytes(int K, int C) { return (size_t)q4_tiles(K) * q4_blocks(C) * 1024; }
+inline size_t q4_scale_bytes(int K, int C, int group) { return (size_t)q4_tiles(K) * q4_blocks(C) * (kQ4Block / group) * 64; }
+// codes: K x ceil(C/2) bytes; zeros: NULL or K x ceil(C/group) bytes; *flag (device, cleared by the launch) becomes 1 if a zero point is above 15
+hipError_t launch_q4_import(const fscnn_q4 *q, const unsigned char *codes, const void *scales, const unsigned char *zeros, int *flag, hipStream_t st);
+hipError_t launch_q4_compress(const fscnn_q4 *q, const void *w, int type, long long ldw, hipStream_t st);
+// the inverse of launch_q4_import; zeros: NULL, or written
+hipError_t launch_q4_export(const fscnn_q4 *q, unsigned char *codes, void *scales, unsigned char *zeros, hipStream_t st);
+
+// ---- q4_linear.hip
+hipError_t launch_linear_q4(const fscnn_q4 *q, const void *x, int x_type, long long ldx, const float *x_scale, int x_scale_cols, int M,
+                            const float *bias, int act, void *y, int y_type, long long ldy, hipStream_t st);
+
+// ---- rms_norm.hip
+constexpr int kNormMaxD = 65536;
+hipError_t launch_rms_norm(const void *x, int type, long long ldx, const void *residual, long long ldr, void *residual_out, long long ldo,
+                           const void *weight, int weight_type, int M, int D, float eps, void *y, int y_type, long long ldy, float *scale,
+                           int group, hipStream_t st);
 
 // ---- compress.hip
 // cnt: K + scan_tmp_elems(K) ints; rowptr: K + 2, the last one for the stored values of the filter that stores the fewest, of those that store

@@ -23,13 +23,15 @@ static struct {
     __typeof__(&fscnn_input_info) input_info;
     __typeof__(&fscnn_sparse_transpose) transpose;
     __typeof__(&fscnn_sparse_tensor_transpose) tensor_transpose;
+    __typeof__(&fscnn_linear_q4) linear_q4;
+    __typeof__(&fscnn_rms_norm) rms_norm;
 } L;
 
 static const char *const kNames[] = {
     "fscnn_conv2d_sparse_filter_ex", "fscnn_conv2d_sparse_filter_pool2x2", "fscnn_conv2d_sparse_filter_leaky",
     "fscnn_conv2d_sparse_filter_emit", "fscnn_conv2d_sparse_filter_emit_into", "fscnn_conv2d_sparse_input",
     "fscnn_conv2d_sparse_input_prepared", "fscnn_filter_compress", "fscnn_filter_info", "fscnn_input_compress",
-    "fscnn_input_info", "fscnn_sparse_transpose", "fscnn_sparse_tensor_transpose",
+    "fscnn_input_info", "fscnn_sparse_transpose", "fscnn_sparse_tensor_transpose", "fscnn_linear_q4", "fscnn_rms_norm",
 };
 enum { kEntries = sizeof(kNames) / sizeof(kNames[0]) };
 _Static_assert(sizeof(L) == kEntries * sizeof(void *), "one name per entry point");
@@ -58,6 +60,18 @@ static void *getp(PyObject *o, int *bad)
     void *p = PyLong_AsVoidPtr(o);
     if (!p && PyErr_Occurred()) *bad = 1;
     return p;
+}
+static long long getll(PyObject *o, int *bad)
+{
+    const long long v = PyLong_AsLongLong(o);
+    if (v == -1 && PyErr_Occurred()) *bad = 1;
+    return v;
+}
+static float getf(PyObject *o, int *bad)
+{
+    const double d = PyFloat_AsDouble(o);
+    if (d == -1.0 && PyErr_Occurred()) *bad = 1;
+    return (float)d;
 }
 static int wrong_count(Py_ssize_t n, Py_ssize_t want)
 {
@@ -207,11 +221,57 @@ static PyObject *py_transpose(PyObject *self, PyObject *const *a, Py_ssize_t n)
     return PyLong_FromLong(st);
 }
 
+/* linear_q4(q, x, x_type, ldx, x_scale, x_scale_cols, M, C, bias, slope, y, y_type, ldy, stream) -> status */
+static PyObject *py_linear_q4(PyObject *self, PyObject *const *a, Py_ssize_t n)
+{
+    if (wrong_count(n, 14)) return NULL;
+    int bad = 0, st = 0;
+    void *q = getp(a[0], &bad), *x = getp(a[1], &bad);
+    const int xt = geti(a[2], &bad);
+    const long long ldx = getll(a[3], &bad);
+    void *xs = getp(a[4], &bad);
+    const int cols = geti(a[5], &bad), M = geti(a[6], &bad), C = geti(a[7], &bad);
+    void *b = getp(a[8], &bad);
+    const float slope = getf(a[9], &bad);
+    void *y = getp(a[10], &bad);
+    const int yt = geti(a[11], &bad);
+    const long long ldy = getll(a[12], &bad);
+    void *s = getp(a[13], &bad);
+    CALL(L.linear_q4(q, x, xt, ldx, xs, cols, M, C, b, slope, y, yt, ldy, s));
+    return PyLong_FromLong(st);
+}
+
+/* rms_norm(x, x_type, ldx, residual, ldr, residual_out, ldo, weight, weight_type, M, D, eps, y, y_type, ldy, scale, group, stream) -> status */
+static PyObject *py_rms_norm(PyObject *self, PyObject *const *a, Py_ssize_t n)
+{
+    if (wrong_count(n, 18)) return NULL;
+    int bad = 0, st = 0;
+    void *x = getp(a[0], &bad);
+    const int xt = geti(a[1], &bad);
+    const long long ldx = getll(a[2], &bad);
+    void *r = getp(a[3], &bad);
+    const long long ldr = getll(a[4], &bad);
+    void *ro = getp(a[5], &bad);
+    const long long ldo = getll(a[6], &bad);
+    void *w = getp(a[7], &bad);
+    const int wt = geti(a[8], &bad), M = geti(a[9], &bad), D = geti(a[10], &bad);
+    const float eps = getf(a[11], &bad);
+    void *y = getp(a[12], &bad);
+    const int yt = geti(a[13], &bad);
+    const long long ldy = getll(a[14], &bad);
+    void *sc = getp(a[15], &bad);
+    const int group = geti(a[16], &bad);
+    void *s = getp(a[17], &bad);
+    CALL(L.rms_norm(x, xt, ldx, r, ldr, ro, ldo, w, wt, M, D, eps, y, yt, ldy, sc, group, s));
+    return PyLong_FromLong(st);
+}
+
 #define FAST(name, fn) {name, (PyCFunction)(void (*)(void))fn, METH_FASTCALL, NULL}
 static PyMethodDef methods[] = {
     {"bind", py_bind, METH_O, NULL},
     FAST("conv", py_conv), FAST("emit", py_emit), FAST("conv_si", py_conv_si), FAST("conv_sip", py_conv_sip),
     FAST("compress", py_compress), FAST("transpose", py_transpose),
+    FAST("linear_q4", py_linear_q4), FAST("rms_norm", py_rms_norm),
     {NULL, NULL, 0, NULL},
 };
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fscnn_call", NULL, -1, methods, NULL, NULL, NULL, NULL};

@@ -36,6 +36,8 @@ EXPORTS = [
     "fscnn_dense_filter_prepare", "fscnn_dense_filter_destroy", "fscnn_conv2d_sparse_input_prepared",
     "fscnn_si_variant_count", "fscnn_conv2d_sparse_filter_leaky", "fscnn_sparse_transpose_noalloc",
     "fscnn_filter_prepare_ex", "fscnn_sf_band_choice", "fscnn_sf_contract_choice", "fscnn_sf_split_choice", "fscnn_sf_serves", "fscnn_si_contract_choice", "fscnn_si_split_choice", "fscnn_pool_trim",
+    "fscnn_q4_compress", "fscnn_q4_import", "fscnn_q4_info", "fscnn_q4_export", "fscnn_q4_destroy",
+    "fscnn_linear_q4", "fscnn_rms_norm",
 ]
 
 NCHW, N4 = 0, 1      # fscnn_layout_t
@@ -613,3 +615,194 @@ def sparse_tensor_transpose(rowptr, widx, val, W, H, C, workspace=None):
     if rowptr.numel() != C * H + 1:
         raise TypeError("rowptr must have C*H + 1 elements")
     return _transpose("fscnn_sparse_tensor_transpose", rowptr, widx, val, (W, H, C), W * H, workspace)
+
+
+# ---------------------------------------------------------------- weights in 4 bits, and the norm in front of them
+F32, F16, BF16, I8 = range(4)        # fscnn_dtype_t
+_DTYPES = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16, torch.int8: I8}
+_FLOATS = (torch.float32, torch.float16, torch.bfloat16)
+
+
+def _rows(t, name, types, shape=None):
+    """Checks a matrix on the current device whose rows may lie apart."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype in types and t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] <= 1)):
+        raise TypeError("%s must be a 2-D CUDA tensor of type %s with adjacent elements in a row" % (name, " or ".join(map(str, types))))
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise TypeError("%s must be %s" % (name, " x ".join(map(str, shape))))
+    if t.device.index != torch._C._cuda_getDevice():
+        raise TypeError("%s is not on the current device" % name)
+    return t
+
+
+def _vector(t, name, types, n):
+    if t is None:
+        return None
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype in types and t.is_contiguous() and t.numel() == n):
+        raise TypeError("%s must be a contiguous CUDA tensor of type %s with %d elements" % (name, " or ".join(map(str, types)), n))
+    if t.device.index != torch._C._cuda_getDevice():
+        raise TypeError("%s is not on the current device" % name)
+    return t
+
+
+def _ld(t):
+    """Distance of a matrix's rows in elements (a single row's stride says nothing)."""
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+class Q4Weights:
+    """Owner of a fscnn_q4_t handle: K x C weights in 4 bits, a scale (and zero point) for each group of columns."""
+
+    def __init__(self, handle, shape, group, zeros, scale_dtype):
+        self._h = handle
+        self.shape = shape
+        self.group = group
+        self.zeros = zeros
+        self.scale_dtype = scale_dtype
+
+    def __del__(self):
+        try:
+            self.destroy()
+        except Exception:        # interpreter shutdown: the module's globals may be gone already
+            pass
+
+    def destroy(self):
+        if getattr(self, "_h", None):
+            lib().fscnn_q4_destroy(self._h)
+            self._h = None
+
+    @property
+    def handle(self):
+        if not self._h:
+            raise RuntimeError("4-bit weights already destroyed")
+        return self._h
+
+    @property
+    def address(self):
+        return self.handle.value
+
+
+def q4_compress(w, group=128, zeros=False):
+    """fscnn_q4_compress: dense K x C CUDA tensor (float32, float16, bfloat16) -> Q4Weights; zeros: with a zero point per group
+    (else codes around 8)."""
+    w = _rows(w, "w", _FLOATS)
+    K, C = w.shape
+    h = ctypes.c_void_p()
+    _check(lib().fscnn_q4_compress(_ptr(w), _i(_DTYPES[w.dtype]), _i(K), _i(C), ctypes.c_longlong(_ld(w)), _i(group), _i(1 if zeros else 0),
+                                   _stream(), ctypes.byref(h)), "fscnn_q4_compress")
+    return Q4Weights(h, (K, C), int(group), bool(zeros), torch.float16 if w.dtype == torch.float16 else torch.bfloat16)
+
+
+def q4_import(codes, scales, zeros=None, group=128, c=None):
+    """fscnn_q4_import: codes uint8 K x ceil(c/2) (even column in the low four bits; c defaults to twice the bytes), scales float16 or
+    bfloat16 K x ceil(c/group), zeros uint8 of the same shape or None (8) -> Q4Weights."""
+    codes = _rows(codes, "codes", (torch.uint8,))
+    K = codes.shape[0]
+    C = 2 * codes.shape[1] if c is None else int(c)
+    if (C + 1) // 2 != codes.shape[1]:
+        raise TypeError("codes must be K x ceil(c/2)")
+    if group not in (32, 64, 128):
+        raise FscnnError(4, "fscnn_q4_import")
+    ng = (C + group - 1) // group
+    _rows(scales, "scales", (torch.float16, torch.bfloat16), (K, ng))
+    if zeros is not None:
+        _rows(zeros, "zeros", (torch.uint8,), (K, ng))
+    if not all(t is None or t.is_contiguous() for t in (codes, scales, zeros)):
+        raise TypeError("codes, scales and zeros must be contiguous")
+    h = ctypes.c_void_p()
+    _check(lib().fscnn_q4_import(_ptr(codes), _ptr(scales), _i(_DTYPES[scales.dtype]), _ptr(zeros), _i(K), _i(C), _i(group), _stream(),
+                                 ctypes.byref(h)), "fscnn_q4_import")
+    return Q4Weights(h, (K, C), int(group), zeros is not None, scales.dtype)
+
+
+def q4_export(q):
+    """fscnn_q4_export -> CPU tensors (codes uint8 K x ceil(C/2), scales K x ceil(C/group), zeros uint8 K x ceil(C/group))."""
+    K, C = q.shape
+    ng = (C + q.group - 1) // q.group
+    codes, zeros = torch.empty(K, (C + 1) // 2, dtype=torch.uint8), torch.empty(K, ng, dtype=torch.uint8)
+    scales = torch.empty(K, ng, dtype=q.scale_dtype)
+    _check(lib().fscnn_q4_export(q.handle, _ptr(codes), _ptr(scales), _ptr(zeros)), "fscnn_q4_export")
+    return codes, scales, zeros
+
+
+def linear_q4(q, x, bias=None, relu=False, leaky=None, out=None, out_dtype=None, x_scale=None):
+    """fscnn_linear_q4: x M x C -> act(x W^T + bias), M x K.  x float32, float16 or bfloat16, or int8 with x_scale (float32; M: a scale
+    per row, M x ceil(C/group): one per row and group).  The result has out's type, or out_dtype, or x's (float32 for int8).  Rows of x and out
+    may lie apart."""
+    x = _rows(x, "x", tuple(_DTYPES))
+    M, C = x.shape
+    K, group = q.shape[0], q.group
+    cols = 1
+    if x.dtype == torch.int8:
+        if x_scale is None:
+            raise TypeError("int8 x needs x_scale")
+        if isinstance(x_scale, torch.Tensor) and x_scale.dim() == 2:
+            cols = x_scale.shape[1]
+            if cols != 1 and cols != (C + group - 1) // group:
+                raise TypeError("x_scale must have one column, or one for each group of the weights")
+        _vector(x_scale, "x_scale", (torch.float32,), M * cols)
+        want = torch.float32
+    else:
+        if x_scale is not None:
+            raise TypeError("x_scale belongs to int8 x")
+        want = x.dtype
+    if out is None:
+        out = x.new_empty((M, K), dtype=want if out_dtype is None else out_dtype)
+        if out.dtype not in _FLOATS:
+            raise TypeError("out_dtype must be float32, float16 or bfloat16")
+    else:
+        _rows(out, "out", _FLOATS if out_dtype is None else (out_dtype,), (M, K))
+    _vector(bias, "bias", (torch.float32,), K)
+    if leaky is not None:
+        if relu:
+            raise TypeError("leaky excludes relu")
+        slope = leaky
+    else:
+        slope = 0.0 if relu else 1.0
+    st = _native().linear_q4(q.address, x.data_ptr(), _DTYPES[x.dtype], _ld(x), _addr(x_scale), cols, M, C, _addr(bias), slope, out.data_ptr(),
+                             _DTYPES[out.dtype], _ld(out), _raw_stream())
+    if st != OK:
+        raise FscnnError(st, "fscnn_linear_q4")
+    return out
+
+
+def _norm(x, weight, eps, residual, residual_out, out, scale, group):
+    M, D = x.shape
+    if weight is not None:
+        _vector(weight, "weight", _FLOATS, D)
+    ldr = ldo = 0
+    if residual is not None:
+        _rows(residual, "residual", (x.dtype,), (M, D))
+        ldr = _ld(residual)
+        residual_out = torch.empty_like(residual) if residual_out is None else _rows(residual_out, "residual_out", (x.dtype,), (M, D))
+        ldo = _ld(residual_out)
+    elif residual_out is not None:
+        raise TypeError("residual_out belongs to a residual")
+    st = _native().rms_norm(x.data_ptr(), _DTYPES[x.dtype], _ld(x), _addr(residual), ldr, _addr(residual_out), ldo, _addr(weight),
+                            F32 if weight is None else _DTYPES[weight.dtype], M, D, eps, out.data_ptr(), _DTYPES[out.dtype], _ld(out), _addr(scale),
+                            group, _raw_stream())
+    if st != OK:
+        raise FscnnError(st, "fscnn_rms_norm")
+    return residual_out
+
+
+def rms_norm(x, weight=None, eps=1e-6, residual=None, residual_out=None, out=None):
+    """fscnn_rms_norm: h = x (+ residual), y = h / sqrt(mean(h^2) + eps) * weight for M x D x -> y, or (y, h) with a residual.  h goes to
+    residual_out (a new tensor if None; it may be residual or x itself), y to out (any floating type; it may be x)."""
+    x = _rows(x, "x", _FLOATS)
+    out = x.new_empty(x.shape) if out is None else _rows(out, "out", _FLOATS, x.shape)
+    h = _norm(x, weight, eps, residual, residual_out, out, None, 0)
+    return out if residual is None else (out, h)
+
+
+def rms_norm_q8(x, weight=None, eps=1e-6, residual=None, residual_out=None, group=0, out=None, scale=None):
+    """The same with y in int8: -> (y, scale), or (y, scale, h) with a residual.  group 0: a scale per row (M); 32, 64, 128: one per row
+    and group (M x ceil(D/group)), as linear_q4 takes them."""
+    x = _rows(x, "x", _FLOATS)
+    M, D = x.shape
+    if group not in (0, 32, 64, 128):
+        raise FscnnError(4, "fscnn_rms_norm")
+    out = x.new_empty(x.shape, dtype=torch.int8) if out is None else _rows(out, "out", (torch.int8,), x.shape)
+    shape = (M, (D + group - 1) // group) if group else (M,)
+    scale = x.new_empty(shape, dtype=torch.float32) if scale is None else _vector(scale, "scale", (torch.float32,), M * (shape[1] if group else 1))
+    h = _norm(x, weight, eps, residual, residual_out, out, scale, group)
+    return (out, scale) if residual is None else (out, scale, h)
