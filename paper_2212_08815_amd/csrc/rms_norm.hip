@@ -1,5 +1,10 @@
-// Root-mean-square norm with the residual's addition and, if wanted, an output in 8 bits with scales.  The simple form: a work-group of 1024
-// threads per row, the row in registers.
+// Root-mean-square norm with the residual's addition and, if wanted, an output in 8 bits with scales:
+//   h = x + r,  y = h / sqrt(mean(h^2) + eps) * w,  scale = max|y| / 127,  code = rint(y / scale)
+//
+// One pass: a row stays in registers between the sum of its squares and its outputs, so that x and r are read and y and h written once (8 bytes an
+// element in 16 bits), and memory bounds all but the smallest calls.  TH threads take a row: a wave up to 16 vectors' worth of
+// columns a lane, so that no barrier is met, more threads for longer rows.  A thread holds N vectors of 16 bytes, vector i of a row at thread
+// i mod TH, and issues all loads of its row before it uses the first.  A group of 32 to 128 columns lies in 4 to 32 adjacent lanes.
 #include <type_traits>
 
 #include "internal.h"
@@ -10,15 +15,13 @@ namespace fscnn {
 namespace {
 
 struct NormArgs {
-    const void *x, *r, *w;
-    void *ro, *y;
+    const char *x, *r, *w;
+    char *ro, *y;
     float *scale;
-    long long ldx, ldr, ldo, ldy;
-    int type, w_type, y_type, M, D, group;
+    long long ldx, ldr, ldo, ldy;              // in bytes
+    int w_type, y_type, M, D, group;
     float eps;
 };
-
-constexpr int kThreads = 1024;
 
 // |v| as a number that orders as it does, NaN above all
 __device__ inline uint32_t magnitude(float v) { return __builtin_bit_cast(uint32_t, v) & 0x7fffffffu; }
@@ -32,89 +35,189 @@ __device__ inline float scale_of(uint32_t most, float *up, float *inv)
     return a / 127.0f;
 }
 
-__device__ inline int8_t code_of(float y, float up, float inv)
+__device__ inline uint32_t code_of(float y, float up, float inv)
 {
-    return inv > 0.0f ? (int8_t)(int)fminf(fmaxf(rintf(y * up * inv), -127.0f), 127.0f) : (int8_t)0;   // (y * 0 may be NaN)
+    return inv > 0.0f ? (uint32_t)(int)fminf(fmaxf(rintf(y * up * inv), -127.0f), 127.0f) & 255u : 0u;   // (y * 0 may be NaN)
 }
 
-template <int N> __global__ void __launch_bounds__(kThreads) rms_norm_kernel(const NormArgs a)
+// V elements of type T from column c of a row on, as they are; zeros from D on
+template <int T, int V> struct Vec { typename Elem<T>::type e[V]; };
+template <int T, int V> __device__ inline Vec<T, V> load_vec(const char *row, int c, int D)
 {
-    __shared__ float sums[kThreads / 64];
-    __shared__ uint32_t mags[kThreads / 64];
-    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
-    for (int m = blockIdx.x; m < a.M; m += gridDim.x) {
-        float h[N], sum = 0.0f;
+    using E = typename Elem<T>::type;
+    Vec<T, V> v;
+    if (c + V <= D) __builtin_memcpy(&v, row + (long long)c * (int)sizeof(E), sizeof(v));
+    else
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int c = i * kThreads + t;
-            h[i] = 0.0f;
-            if (c < a.D) {
-                h[i] = load_float(a.x, m * a.ldx + c, a.type);
-                if (a.r) h[i] += load_float(a.r, m * a.ldr + c, a.type);
-                if (a.ro) store_float(a.ro, m * a.ldo + c, a.type, h[i]);
-            }
-            sum = __builtin_fmaf(h[i], h[i], sum);
+        for (int j = 0; j < V; ++j) {
+            v.e[j] = E{};
+            if (c + j < D) v.e[j] = reinterpret_cast<const E *>(row)[c + j];
         }
-        for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
-        __syncthreads();
+    return v;
+}
+
+template <int T, int V> __device__ inline void store_vec(char *row, int c, int D, const float *f)
+{
+    using E = typename Elem<T>::type;
+    Vec<T, V> v;
+#pragma unroll
+    for (int j = 0; j < V; ++j) v.e[j] = (E)f[j];
+    if (c + V <= D) __builtin_memcpy(row + (long long)c * (int)sizeof(E), &v, sizeof(v));
+    else
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+            if (c + j < D) reinterpret_cast<E *>(row)[c + j] = v.e[j];
+}
+
+template <int V> __device__ inline void store_any(char *row, int type, int c, int D, const float *f)
+{
+    if (type == FSCNN_F32) store_vec<FSCNN_F32, V>(row, c, D, f);
+    else if (type == FSCNN_F16) store_vec<FSCNN_F16, V>(row, c, D, f);
+    else store_vec<FSCNN_BF16, V>(row, c, D, f);
+}
+
+template <int V> __device__ inline void store_codes(char *row, int c, int D, const float *f, float up, float inv)
+{
+    uint32_t w[V / 4];
+#pragma unroll
+    for (int i = 0; i < V / 4; ++i) {
+        w[i] = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[i] |= code_of(f[4 * i + j], up, inv) << (8 * j);
+    }
+    if (c + V <= D) __builtin_memcpy(row + c, w, V);
+    else
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+            if (c + j < D) row[c + j] = (char)(w[j / 4] >> (8 * (j % 4)));
+}
+
+template <int T, int N, int TH> __global__ void __launch_bounds__(TH < 256 ? 256 : TH) rms_norm_kernel(const NormArgs a)
+{
+    constexpr int V = 16 / (int)sizeof(typename Elem<T>::type), kWaves = TH / 64, kRows = TH < 256 ? 256 / TH : 1;
+    __shared__ float sums[kWaves];
+    __shared__ uint32_t mags[kWaves];
+    const int t = TH < 256 ? threadIdx.x % TH : threadIdx.x, lane = threadIdx.x & 63, wave = t >> 6;
+    const long long m = (long long)blockIdx.x * kRows + (TH < 256 ? threadIdx.x / TH : 0);
+    if (m >= a.M) return;                      // (with more than one row a work-group, rows meet no barrier)
+    const char *x = a.x + m * a.ldx, *r = a.r + m * a.ldr;
+    Vec<T, V> xv[N], rv[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) xv[i] = load_vec<T, V>(x, (i * TH + t) * V, a.D);
+    if (a.r)
+#pragma unroll
+        for (int i = 0; i < N; ++i) rv[i] = load_vec<T, V>(r, (i * TH + t) * V, a.D);
+    float h[N][V], sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            h[i][j] = (float)xv[i].e[j];
+            if (a.r) h[i][j] += (float)rv[i].e[j];
+            sum = __builtin_fmaf(h[i][j], h[i][j], sum);
+        }
+        if (a.ro) store_vec<T, V>(a.ro + m * a.ldo, (i * TH + t) * V, a.D, h[i]);
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
+    if constexpr (kWaves > 1) {
         if (lane == 0) sums[wave] = sum;
         __syncthreads();
         sum = 0.0f;
-        for (int i = 0; i < kThreads / 64; ++i) sum += sums[i];
-        const float f = 1.0f / sqrtf(sum / (float)a.D + a.eps);
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int c = i * kThreads + t;
-            if (c < a.D) h[i] = h[i] * f * (a.w ? load_float(a.w, c, a.w_type) : 1.0f);
-        }
-        if (a.y_type != FSCNN_I8) {
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const int c = i * kThreads + t;
-                if (c < a.D) store_float(a.y, m * a.ldy + c, a.y_type, h[i]);
-            }
-            continue;
-        }
-        int8_t *y = static_cast<int8_t *>(a.y) + m * a.ldy;
-        float up, inv;
-        if (a.group == 0) {
-            uint32_t most = 0;
-#pragma unroll
-            for (int i = 0; i < N; ++i)
-                if (i * kThreads + t < a.D) most = max(most, magnitude(h[i]));
-            for (int d = 1; d < 64; d *= 2) most = max(most, (uint32_t)__shfl_xor((int)most, d));
-            if (lane == 0) mags[wave] = most;
-            __syncthreads();
-            most = 0;
-            for (int i = 0; i < kThreads / 64; ++i) most = max(most, mags[i]);
-            const float s = scale_of(most, &up, &inv);
-            if (t == 0) a.scale[m] = s;
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const int c = i * kThreads + t;
-                if (c < a.D) y[c] = code_of(h[i], up, inv);
-            }
-            continue;
-        }
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int c = i * kThreads + t;
-            uint32_t most = c < a.D ? magnitude(h[i]) : 0;
-            for (int d = 1; d < 32; d *= 2) most = max(most, (uint32_t)__shfl_xor((int)most, d));
-            if (a.group >= 64) most = max(most, (uint32_t)__shfl_xor((int)most, 32));
-            if (a.group == 128) {          // two waves
-                __syncthreads();
-                if (lane == 0) mags[wave] = most;
-                __syncthreads();
-                most = max(mags[wave], mags[wave ^ 1]);
-            }
-            const float s = scale_of(most, &up, &inv);
-            if (c < a.D) {
-                y[c] = code_of(h[i], up, inv);
-                if (c % a.group == 0) a.scale[m * (long long)((a.D + a.group - 1) / a.group) + c / a.group] = s;
-            }
-        }
+        for (int i = 0; i < kWaves; ++i) sum += sums[i];
     }
+    const float f = 1.0f / sqrtf(sum / (float)a.D + a.eps);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int c = (i * TH + t) * V;
+        float w[V];
+        if (!a.w) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) w[j] = 1.0f;
+        } else if (a.w_type == FSCNN_F32) {
+            const auto v = load_vec<FSCNN_F32, V>(a.w, c, a.D);
+#pragma unroll
+            for (int j = 0; j < V; ++j) w[j] = v.e[j];
+        } else if (a.w_type == FSCNN_F16) {
+            const auto v = load_vec<FSCNN_F16, V>(a.w, c, a.D);
+#pragma unroll
+            for (int j = 0; j < V; ++j) w[j] = (float)v.e[j];
+        } else {
+            const auto v = load_vec<FSCNN_BF16, V>(a.w, c, a.D);
+#pragma unroll
+            for (int j = 0; j < V; ++j) w[j] = (float)v.e[j];
+        }
+#pragma unroll
+        for (int j = 0; j < V; ++j) h[i][j] = h[i][j] * f * w[j];   // (columns from D on: zeros, or NaN; they are not stored and not measured)
+    }
+    char *y = a.y + m * a.ldy;
+    if (a.y_type != FSCNN_I8) {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if ((i * TH + t) * V < a.D) store_any<V>(y, a.y_type, (i * TH + t) * V, a.D, h[i]);
+        return;
+    }
+    uint32_t most[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        most[i] = 0;
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+            if ((i * TH + t) * V + j < a.D) most[i] = max(most[i], magnitude(h[i][j]));
+    }
+    float up, inv;
+    if (a.group == 0) {
+#pragma unroll
+        for (int i = 1; i < N; ++i) most[0] = max(most[0], most[i]);
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) most[0] = max(most[0], (uint32_t)__shfl_xor((int)most[0], d));
+        if constexpr (kWaves > 1) {
+            if (lane == 0) mags[wave] = most[0];
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < kWaves; ++i) most[0] = max(most[0], mags[i]);
+        }
+        const float s = scale_of(most[0], &up, &inv);
+        if (t == 0) a.scale[m] = s;
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if ((i * TH + t) * V < a.D) store_codes<V>(y, (i * TH + t) * V, a.D, h[i], up, inv);
+        return;
+    }
+    const int ng = (a.D + a.group - 1) / a.group;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        for (int d = 1; d * V < a.group; d *= 2) most[i] = max(most[i], (uint32_t)__shfl_xor((int)most[i], d));
+        const float s = scale_of(most[i], &up, &inv);
+        const int c = (i * TH + t) * V;
+        if (c >= a.D) continue;
+        if (c % a.group == 0) a.scale[m * ng + c / a.group] = s;
+        store_codes<V>(y, c, a.D, h[i], up, inv);
+    }
+}
+
+template <int T, int N, int TH> hipError_t launch_rows(const NormArgs &a, hipStream_t st)
+{
+    constexpr int rows = TH < 256 ? 256 / TH : 1;
+    const long long grid = ((long long)a.M + rows - 1) / rows, threads = TH < 256 ? 256 : TH;
+    if (grid * threads > 0xffffffffLL) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((rms_norm_kernel<T, N, TH>), dim3((unsigned)grid), dim3((unsigned)threads), 0, st, a);
+    return hipGetLastError();
+}
+
+template <int T> hipError_t launch_type(const NormArgs &a, hipStream_t st)
+{
+    constexpr int V = 16 / (int)sizeof(typename Elem<T>::type);
+    const int n = (a.D + V - 1) / V;           // vectors of a row
+    if (n <= 64) return launch_rows<T, 1, 64>(a, st);
+    if (n <= 128) return launch_rows<T, 2, 64>(a, st);
+    if (n <= 256) return launch_rows<T, 1, 256>(a, st);
+    if (n <= 512) return launch_rows<T, 2, 256>(a, st);
+    if (n <= 1024) return launch_rows<T, 4, 256>(a, st);
+    if (n <= 4096) return launch_rows<T, 4, 1024>(a, st);
+    if (n <= 8192) return launch_rows<T, 8, 1024>(a, st);
+    return launch_rows<T, 16, 1024>(a, st);    // (fp32 past 32768 columns)
 }
 
 }  // namespace
@@ -123,13 +226,19 @@ hipError_t launch_rms_norm(const void *x, int type, long long ldx, const void *r
                            const void *weight, int weight_type, int M, int D, float eps, void *y, int y_type, long long ldy, float *scale,
                            int group, hipStream_t st)
 {
-    const NormArgs a = {x, residual, weight, residual_out, y, scale, ldx, ldr, ldo, ldy, type, weight_type, y_type, M, D, group, eps};
-    const dim3 grid(M < 65536 ? M : 65536), block(kThreads);
-    if (D <= 4096) hipLaunchKernelGGL(rms_norm_kernel<4>, grid, block, 0, st, a);
-    else if (D <= 16384) hipLaunchKernelGGL(rms_norm_kernel<16>, grid, block, 0, st, a);
-    else if (D <= kNormMaxD) hipLaunchKernelGGL(rms_norm_kernel<64>, grid, block, 0, st, a);
-    else return hipErrorInvalidValue;
-    return hipGetLastError();
+    if (D > kNormMaxD) return hipErrorInvalidValue;
+    const int e = type == FSCNN_F32 ? 4 : 2, ey = y_type == FSCNN_F32 ? 4 : y_type == FSCNN_I8 ? 1 : 2;
+    // rows in launches that a grid holds
+    constexpr long long kMost = 1 << 20;
+    for (long long m = 0; m < M; m += kMost) {
+        const NormArgs a = {static_cast<const char *>(x) + m * ldx * e, residual ? static_cast<const char *>(residual) + m * ldr * e : nullptr,
+                            static_cast<const char *>(weight), residual_out ? static_cast<char *>(residual_out) + m * ldo * e : nullptr,
+                            static_cast<char *>(y) + m * ldy * ey, scale ? scale + m * (group ? (D + group - 1) / group : 1) : nullptr, ldx * e, ldr * e,
+                            ldo * e, ldy * ey, weight_type, y_type, (int)(M - m < kMost ? M - m : kMost), D, group, eps};
+        const hipError_t err = with_type(type, [&](auto t) { return launch_type<decltype(t)::value>(a, st); });
+        if (err != hipSuccess) return err;
+    }
+    return hipSuccess;
 }
 
 }  // namespace fscnn
