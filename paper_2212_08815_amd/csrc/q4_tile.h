@@ -15,7 +15,10 @@ namespace fscnn {
 typedef uint32_t u2v __attribute__((ext_vector_type(2)));
 typedef uint32_t u4v __attribute__((ext_vector_type(4)));
 typedef float q4f4 __attribute__((ext_vector_type(4)));
+typedef float q4f2 __attribute__((ext_vector_type(2)));
+typedef float q4f16 __attribute__((ext_vector_type(16)));
 typedef int q4i4 __attribute__((ext_vector_type(4)));
+typedef int q4i16 __attribute__((ext_vector_type(16)));
 typedef __bf16 q4b2 __attribute__((ext_vector_type(2)));
 typedef __bf16 q4b8 __attribute__((ext_vector_type(8)));
 typedef _Float16 q4h2 __attribute__((ext_vector_type(2)));
@@ -39,6 +42,18 @@ template <> struct XOp<FSCNN_BF16> {
         o[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 512.0f, true));
         return o;
     }
+    using Zero = float;
+    __device__ static Zero zero(uint32_t word) { return (float)(word & 15); }
+    __device__ static Op weights(uint32_t w, Zero z)
+    {
+        const int lo = w & 0x0f0f0f0f, hi = w >> 4 & 0x0f0f0f0f;
+        const q4f2 f[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp8(lo, 512.0f, false), __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(lo, 512.0f, true),
+                           __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(hi, 512.0f, false), __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(hi, 512.0f, true)};
+        Op o;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] = __builtin_bit_cast(uint32_t, q4b2{(__bf16)(f[i][0] - z), (__bf16)(f[i][1] - z)});
+        return o;
+    }
     __device__ static Op ones() { return Op{0x3f803f80, 0x3f803f80, 0x3f803f80, 0x3f803f80}; }
     __device__ static Acc mfma(const Op &a, const Op &b, const Acc &c)
     {
@@ -59,6 +74,19 @@ template <> struct XOp<FSCNN_F16> {
         o[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 512.0f, true));
         o[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 512.0f, false));
         o[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 512.0f, true));
+        return o;
+    }
+    using Zero = q4h2;
+    __device__ static Zero zero(uint32_t word) { return Zero{(_Float16)(float)(word & 15), (_Float16)(float)(word & 15)}; }
+    __device__ static Op weights(uint32_t w, Zero z)
+    {
+        const Op c = codes(w);
+        Op o;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t pair = c[i];       // (a bit cast of a vector's element itself is read from the vector's start)
+            o[i] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(q4h2, pair) - z);
+        }
         return o;
     }
     __device__ static Op ones() { return Op{0x3c003c00, 0x3c003c00, 0x3c003c00, 0x3c003c00}; }
@@ -90,6 +118,9 @@ template <> struct XOp<FSCNN_F32> {
         }
     }
     __device__ static Op codes(uint32_t w) { return XOp<FSCNN_BF16>::codes(w); }
+    using Zero = float;
+    __device__ static Zero zero(uint32_t word) { return XOp<FSCNN_BF16>::zero(word); }
+    __device__ static Op weights(uint32_t w, Zero z) { return XOp<FSCNN_BF16>::weights(w, z); }
     __device__ static Op ones() { return XOp<FSCNN_BF16>::ones(); }
     __device__ static Acc mfma(const Op &a, const Op &b, const Acc &c) { return XOp<FSCNN_BF16>::mfma(a, b, c); }
 };
@@ -100,6 +131,9 @@ template <> struct XOp<FSCNN_I8> {
     using Acc = q4i4;
     __device__ static void parts(const Raw &r, Op *o) { o[0] = r; }
     __device__ static Op codes(uint32_t w) { return Op{w & 0x0f0f0f0f, w >> 4 & 0x0f0f0f0f}; }
+    using Zero = uint32_t;                    // (128 - z) in every byte: with a code's added, the high bit flipped is what signs it
+    __device__ static Zero zero(uint32_t word) { return (128 - (word & 15)) * 0x01010101u; }
+    __device__ static Op weights(uint32_t w, Zero z) { return Op{((w & 0x0f0f0f0f) + z) ^ 0x80808080u, ((w >> 4 & 0x0f0f0f0f) + z) ^ 0x80808080u}; }
     __device__ static Op ones() { return Op{0x01010101, 0x01010101}; }
     __device__ static Acc mfma(const Op &a, const Op &b, const Acc &c)
     {
