@@ -623,30 +623,38 @@ _DTYPES = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16, torch.i
 _FLOATS = (torch.float32, torch.float16, torch.bfloat16)
 
 
-def _rows(t, name, types, shape=None):
-    """Checks a matrix on the current device whose rows may lie apart."""
-    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype in types and t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] <= 1)):
-        raise TypeError("%s must be a 2-D CUDA tensor of type %s with adjacent elements in a row" % (name, " or ".join(map(str, types))))
-    if shape is not None and tuple(t.shape) != tuple(shape):
-        raise TypeError("%s must be %s" % (name, " x ".join(map(str, shape))))
-    if t.device.index != torch._C._cuda_getDevice():
+def _refuse(t, name, types, what):
+    names = " or ".join(map(str, types))
+    if isinstance(t, torch.Tensor) and t.is_cuda and t.get_device() != torch._C._cuda_getDevice():
         raise TypeError("%s is not on the current device" % name)
-    return t
+    raise TypeError("%s must be a %s of type %s" % (name, what, names))
 
 
-def _vector(t, name, types, n):
-    if t is None:
-        return None
-    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype in types and t.is_contiguous() and t.numel() == n):
-        raise TypeError("%s must be a contiguous CUDA tensor of type %s with %d elements" % (name, " or ".join(map(str, types)), n))
-    if t.device.index != torch._C._cuda_getDevice():
-        raise TypeError("%s is not on the current device" % name)
-    return t
+def _matrix(t, name, types, dev):
+    """(rows, columns, distance of the rows) of a matrix on device `dev` whose rows may lie apart.  (A call's checks cost as much as its
+    launch: few and cheap ones.)"""
+    if not (isinstance(t, torch.Tensor) and t.get_device() == dev and t.dtype in types and t.dim() == 2):
+        _refuse(t, name, types, "2-D CUDA tensor")
+    n, c = t.shape
+    ld, step = t.stride()
+    if step != 1 and c > 1:
+        _refuse(t, name, types, "2-D CUDA tensor with adjacent elements in a row")
+    return n, c, ld if n > 1 else c          # (a single row's stride says nothing)
 
 
-def _ld(t):
-    """Distance of a matrix's rows in elements (a single row's stride says nothing)."""
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+def _first(t, name, types):
+    """The same of a call's first tensor, and the current device, on which it has to be."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda):
+        _refuse(t, name, types, "2-D CUDA tensor")
+    dev = torch._C._cuda_getDevice()
+    n, c, ld = _matrix(t, name, types, dev)
+    return n, c, ld, dev
+
+
+def _vector(t, name, types, n, dev):
+    if not (isinstance(t, torch.Tensor) and t.get_device() == dev and t.dtype in types and t.is_contiguous() and t.numel() == n):
+        _refuse(t, name, types, "contiguous CUDA tensor of %d elements" % n)
+    return t.data_ptr()
 
 
 class Q4Weights:
@@ -684,10 +692,9 @@ class Q4Weights:
 def q4_compress(w, group=128, zeros=False):
     """fscnn_q4_compress: dense K x C CUDA tensor (float32, float16, bfloat16) -> Q4Weights; zeros: with a zero point per group
     (else codes around 8)."""
-    w = _rows(w, "w", _FLOATS)
-    K, C = w.shape
+    K, C, ld, _ = _first(w, "w", _FLOATS)
     h = ctypes.c_void_p()
-    _check(lib().fscnn_q4_compress(_ptr(w), _i(_DTYPES[w.dtype]), _i(K), _i(C), ctypes.c_longlong(_ld(w)), _i(group), _i(1 if zeros else 0),
+    _check(lib().fscnn_q4_compress(_ptr(w), _i(_DTYPES[w.dtype]), _i(K), _i(C), ctypes.c_longlong(ld), _i(group), _i(1 if zeros else 0),
                                    _stream(), ctypes.byref(h)), "fscnn_q4_compress")
     return Q4Weights(h, (K, C), int(group), bool(zeros), torch.float16 if w.dtype == torch.float16 else torch.bfloat16)
 
@@ -695,17 +702,17 @@ def q4_compress(w, group=128, zeros=False):
 def q4_import(codes, scales, zeros=None, group=128, c=None):
     """fscnn_q4_import: codes uint8 K x ceil(c/2) (even column in the low four bits; c defaults to twice the bytes), scales float16 or
     bfloat16 K x ceil(c/group), zeros uint8 of the same shape or None (8) -> Q4Weights."""
-    codes = _rows(codes, "codes", (torch.uint8,))
-    K = codes.shape[0]
-    C = 2 * codes.shape[1] if c is None else int(c)
-    if (C + 1) // 2 != codes.shape[1]:
+    K, nb, _, dev = _first(codes, "codes", (torch.uint8,))
+    C = 2 * nb if c is None else int(c)
+    if (C + 1) // 2 != nb:
         raise TypeError("codes must be K x ceil(c/2)")
     if group not in (32, 64, 128):
         raise FscnnError(4, "fscnn_q4_import")
     ng = (C + group - 1) // group
-    _rows(scales, "scales", (torch.float16, torch.bfloat16), (K, ng))
-    if zeros is not None:
-        _rows(zeros, "zeros", (torch.uint8,), (K, ng))
+    for t, name, types in ((scales, "scales", (torch.float16, torch.bfloat16)), (zeros, "zeros", (torch.uint8,))):
+        if t is not None or name == "scales":
+            if _matrix(t, name, types, dev)[:2] != (K, ng):
+                raise TypeError("%s must be K x ceil(c/group)" % name)
     if not all(t is None or t.is_contiguous() for t in (codes, scales, zeros)):
         raise TypeError("codes, scales and zeros must be contiguous")
     h = ctypes.c_void_p()
@@ -728,58 +735,69 @@ def linear_q4(q, x, bias=None, relu=False, leaky=None, out=None, out_dtype=None,
     """fscnn_linear_q4: x M x C -> act(x W^T + bias), M x K.  x float32, float16 or bfloat16, or int8 with x_scale (float32; M: a scale
     per row, M x ceil(C/group): one per row and group).  The result has out's type, or out_dtype, or x's (float32 for int8).  Rows of x and out
     may lie apart."""
-    x = _rows(x, "x", tuple(_DTYPES))
-    M, C = x.shape
-    K, group = q.shape[0], q.group
-    cols = 1
-    if x.dtype == torch.int8:
+    M, C, ldx, dev = _first(x, "x", _DTYPES)
+    K = q.shape[0]
+    want = x.dtype
+    cols, scale = 1, None
+    if want == torch.int8:
         if x_scale is None:
             raise TypeError("int8 x needs x_scale")
         if isinstance(x_scale, torch.Tensor) and x_scale.dim() == 2:
             cols = x_scale.shape[1]
-            if cols != 1 and cols != (C + group - 1) // group:
+            if cols != 1 and cols != (C + q.group - 1) // q.group:
                 raise TypeError("x_scale must have one column, or one for each group of the weights")
-        _vector(x_scale, "x_scale", (torch.float32,), M * cols)
+        scale = _vector(x_scale, "x_scale", (torch.float32,), M * cols, dev)
         want = torch.float32
-    else:
-        if x_scale is not None:
-            raise TypeError("x_scale belongs to int8 x")
-        want = x.dtype
+    elif x_scale is not None:
+        raise TypeError("x_scale belongs to int8 x")
     if out is None:
-        out = x.new_empty((M, K), dtype=want if out_dtype is None else out_dtype)
-        if out.dtype not in _FLOATS:
-            raise TypeError("out_dtype must be float32, float16 or bfloat16")
+        if out_dtype is not None and out_dtype != want:
+            if out_dtype not in _FLOATS:
+                raise TypeError("out_dtype must be float32, float16 or bfloat16")
+            want = out_dtype
+        out = x.new_empty(M, K) if want == x.dtype else x.new_empty(M, K, dtype=want)
+        ldy = K
     else:
-        _rows(out, "out", _FLOATS if out_dtype is None else (out_dtype,), (M, K))
-    _vector(bias, "bias", (torch.float32,), K)
+        m, k, ldy = _matrix(out, "out", _FLOATS if out_dtype is None else (out_dtype,), dev)
+        if m != M or k != K:
+            raise TypeError("out must be %d x %d" % (M, K))
+        want = out.dtype
+    b = None if bias is None else _vector(bias, "bias", (torch.float32,), K, dev)
     if leaky is not None:
         if relu:
             raise TypeError("leaky excludes relu")
         slope = leaky
     else:
         slope = 0.0 if relu else 1.0
-    st = _native().linear_q4(q.address, x.data_ptr(), _DTYPES[x.dtype], _ld(x), _addr(x_scale), cols, M, C, _addr(bias), slope, out.data_ptr(),
-                             _DTYPES[out.dtype], _ld(out), _raw_stream())
+    st = (_nat or _native()).linear_q4(q.address, x.data_ptr(), _DTYPES[x.dtype], ldx, scale, cols, M, C, b, slope, out.data_ptr(), _DTYPES[want],
+                                       ldy, torch._C._cuda_getCurrentRawStream(dev))
     if st != OK:
         raise FscnnError(st, "fscnn_linear_q4")
     return out
 
 
-def _norm(x, weight, eps, residual, residual_out, out, scale, group):
-    M, D = x.shape
+def _norm(x, weight, eps, residual, residual_out, out, scale, group, dev, M, D, ldx, ldy):
+    w, wt = None, F32
     if weight is not None:
-        _vector(weight, "weight", _FLOATS, D)
+        w, wt = _vector(weight, "weight", _FLOATS, D, dev), _DTYPES[weight.dtype]
+    r = ro = None
     ldr = ldo = 0
     if residual is not None:
-        _rows(residual, "residual", (x.dtype,), (M, D))
-        ldr = _ld(residual)
-        residual_out = torch.empty_like(residual) if residual_out is None else _rows(residual_out, "residual_out", (x.dtype,), (M, D))
-        ldo = _ld(residual_out)
+        n, c, ldr = _matrix(residual, "residual", (x.dtype,), dev)
+        if residual_out is None:
+            residual_out = torch.empty_like(x) if ldx == D else x.new_empty(M, D)
+            ldo = D
+        else:
+            no, co, ldo = _matrix(residual_out, "residual_out", (x.dtype,), dev)
+            if no != M or co != D:
+                raise TypeError("residual_out must be %d x %d" % (M, D))
+        if n != M or c != D:
+            raise TypeError("residual must be %d x %d" % (M, D))
+        r, ro = residual.data_ptr(), residual_out.data_ptr()
     elif residual_out is not None:
         raise TypeError("residual_out belongs to a residual")
-    st = _native().rms_norm(x.data_ptr(), _DTYPES[x.dtype], _ld(x), _addr(residual), ldr, _addr(residual_out), ldo, _addr(weight),
-                            F32 if weight is None else _DTYPES[weight.dtype], M, D, eps, out.data_ptr(), _DTYPES[out.dtype], _ld(out), _addr(scale),
-                            group, _raw_stream())
+    st = (_nat or _native()).rms_norm(x.data_ptr(), _DTYPES[x.dtype], ldx, r, ldr, ro, ldo, w, wt, M, D, eps, out.data_ptr(), _DTYPES[out.dtype], ldy,
+                                      None if scale is None else scale.data_ptr(), group, torch._C._cuda_getCurrentRawStream(dev))
     if st != OK:
         raise FscnnError(st, "fscnn_rms_norm")
     return residual_out
@@ -788,21 +806,33 @@ def _norm(x, weight, eps, residual, residual_out, out, scale, group):
 def rms_norm(x, weight=None, eps=1e-6, residual=None, residual_out=None, out=None):
     """fscnn_rms_norm: h = x (+ residual), y = h / sqrt(mean(h^2) + eps) * weight for M x D x -> y, or (y, h) with a residual.  h goes to
     residual_out (a new tensor if None; it may be residual or x itself), y to out (any floating type; it may be x)."""
-    x = _rows(x, "x", _FLOATS)
-    out = x.new_empty(x.shape) if out is None else _rows(out, "out", _FLOATS, x.shape)
-    h = _norm(x, weight, eps, residual, residual_out, out, None, 0)
+    M, D, ldx, dev = _first(x, "x", _FLOATS)
+    if out is None:
+        out, ldy = torch.empty_like(x) if ldx == D else x.new_empty(M, D), D
+    else:
+        m, d, ldy = _matrix(out, "out", _FLOATS, dev)
+        if m != M or d != D:
+            raise TypeError("out must be %d x %d" % (M, D))
+    h = _norm(x, weight, eps, residual, residual_out, out, None, 0, dev, M, D, ldx, ldy)
     return out if residual is None else (out, h)
 
 
 def rms_norm_q8(x, weight=None, eps=1e-6, residual=None, residual_out=None, group=0, out=None, scale=None):
     """The same with y in int8: -> (y, scale), or (y, scale, h) with a residual.  group 0: a scale per row (M); 32, 64, 128: one per row
     and group (M x ceil(D/group)), as linear_q4 takes them."""
-    x = _rows(x, "x", _FLOATS)
-    M, D = x.shape
+    M, D, ldx, dev = _first(x, "x", _FLOATS)
     if group not in (0, 32, 64, 128):
         raise FscnnError(4, "fscnn_rms_norm")
-    out = x.new_empty(x.shape, dtype=torch.int8) if out is None else _rows(out, "out", (torch.int8,), x.shape)
-    shape = (M, (D + group - 1) // group) if group else (M,)
-    scale = x.new_empty(shape, dtype=torch.float32) if scale is None else _vector(scale, "scale", (torch.float32,), M * (shape[1] if group else 1))
-    h = _norm(x, weight, eps, residual, residual_out, out, scale, group)
+    if out is None:
+        out, ldy = x.new_empty(M, D, dtype=torch.int8), D
+    else:
+        m, d, ldy = _matrix(out, "out", (torch.int8,), dev)
+        if m != M or d != D:
+            raise TypeError("out must be %d x %d" % (M, D))
+    ng = (D + group - 1) // group if group else 1
+    if scale is None:
+        scale = x.new_empty(M, ng, dtype=torch.float32) if group else x.new_empty(M, dtype=torch.float32)
+    else:
+        _vector(scale, "scale", (torch.float32,), M * ng, dev)
+    h = _norm(x, weight, eps, residual, residual_out, out, scale, group, dev, M, D, ldx, ldy)
     return (out, scale) if residual is None else (out, scale, h)
