@@ -482,12 +482,17 @@ fscnn_status_t fscnn_q4_destroy(fscnn_q4_t *q);
  * x_type I8: x[m][c] stands for x_dev[m][c] * x_scale, x_scale_dev M x x_scale_cols floats, one for the row (x_scale_cols 1) or one for
  * each group of the weights (ceil(C/group)); a group's sum is exact in 32-bit integers.
  * An x that is not finite meets every weight of its row, zeros among them; other rows are not touched by it.  M == 0 is no work (pointers
- * to x and y may be NULL then).  y must not overlap x.  Allocates nothing, does not synchronise, needs no scratch; results are run-to-run
- * identical.  Calls on any streams may share a handle.  FSCNN_ERR_MISMATCH if C differs from the handle's, or the current device.
+ * to x and y may be NULL then).  y must not overlap x.  workspace_dev: scratch of fscnn_linear_q4_workspace() bytes, 4-byte aligned, that belongs
+ * to this call until it has run (and to a graph that captured it, as x and y do): the columns are then divided over work-groups, whose
+ * sums lie there; NULL or less is right too, with sums in another order, and slower.  Allocates nothing, does not synchronise; results are
+ * run-to-run identical.  Calls on any streams may share a handle.  FSCNN_ERR_MISMATCH if C differs from the handle's, or the current device.
  * M < 2^31 with M * ldx and M * ldy below 2^62. */
 fscnn_status_t fscnn_linear_q4(const fscnn_q4_t *q, const void *x_dev, fscnn_dtype_t x_type, long long ldx, const float *x_scale_dev,
                                int x_scale_cols, int M, int C, const float *bias_dev, float negative_slope, void *y_dev,
-                               fscnn_dtype_t y_type, long long ldy, void *stream);
+                               fscnn_dtype_t y_type, long long ldy, void *workspace_dev, long long workspace_bytes, void *stream);
+
+/* Bytes of workspace that such a call uses; 0: none, -1: not a live handle, no such type, or M < 0.  Host-only. */
+long long fscnn_linear_q4_workspace(const fscnn_q4_t *q, fscnn_dtype_t x_type, int M);
 
 /* Root-mean-square norm of M rows of D elements, with the residual's addition before it and an 8-bit output behind it:
  *   h = x (+ residual),   y = h / sqrt(mean over the row of h^2 + eps) * weight,

@@ -23,7 +23,7 @@ CSRC = os.path.join(HERE, "csrc")
 OBJDIR = os.path.join(ROOT, "_build")
 LIB = os.path.join(HERE, "libfscnn.so")
 SOURCES = ["api.hip", "compress.hip", "conv_sf.hip", "conv_si.hip", "contract.hip", "contract_split.hip", "pointwise.hip", "transpose.hip",
-           "q4.hip", "q4_linear.hip", "rms_norm.hip"]
+           "q4.hip", "q4_linear.hip", "q4_f32.hip", "q4_f16.hip", "q4_bf16.hip", "q4_i8.hip", "rms_norm.hip"]
 PROBE_LIB = os.path.join(HERE, "libfscnn_bench_probe.so")
 PROBE_SRC = os.path.join(CSRC, "bench_probe.hip")
 CALL_LIB = os.path.join(HERE, "_fscnn_call.so")
@@ -80,7 +80,7 @@ def build_host_sanitized(verbose=True):
 
 def build(force=False, extra_flags=(), verbose=True):
     os.makedirs(OBJDIR, exist_ok=True)
-    headers = [os.path.join(CSRC, "internal.h"), os.path.join(CSRC, "arrival.h"), os.path.join(CSRC, "host_word.h"), os.path.join(CSRC, "lds_dma.h"), os.path.join(CSRC, "lowbits.h"), os.path.join(CSRC, "q4_tile.h"),
+    headers = [os.path.join(CSRC, "internal.h"), os.path.join(CSRC, "arrival.h"), os.path.join(CSRC, "host_word.h"), os.path.join(CSRC, "lds_dma.h"), os.path.join(CSRC, "lowbits.h"), os.path.join(CSRC, "q4_tile.h"), os.path.join(CSRC, "q4_kernels.h"),
                os.path.join(ROOT, "include", "fscnn.h"),
                os.path.abspath(__file__)]
     jobs, objs = [], []

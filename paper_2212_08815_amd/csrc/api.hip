@@ -1766,7 +1766,7 @@ fscnn_status_t fscnn_q4_destroy(fscnn_q4_t *q)
 
 fscnn_status_t fscnn_linear_q4(const fscnn_q4_t *q, const void *x_dev, fscnn_dtype_t x_type, long long ldx, const float *x_scale_dev,
                                int x_scale_cols, int M, int C, const float *bias_dev, float negative_slope, void *y_dev,
-                               fscnn_dtype_t y_type, long long ldy, void *stream)
+                               fscnn_dtype_t y_type, long long ldy, void *workspace_dev, long long workspace_bytes, void *stream)
 {
     if (!q || (M != 0 && (!x_dev || !y_dev))) return FSCNN_ERR_NULL;
     if (!live(q)) return FSCNN_ERR_HANDLE;
@@ -1782,14 +1782,24 @@ fscnn_status_t fscnn_linear_q4(const fscnn_q4_t *q, const void *x_dev, fscnn_dty
     } else if (x_scale_dev) {
         return FSCNN_ERR_UNSUPPORTED;
     }
-    if (misaligned(x_dev, x_type) || misaligned(y_dev, y_type) || misaligned(bias_dev, FSCNN_F32) || x_dev == y_dev) return FSCNN_ERR_UNSUPPORTED;
+    if (misaligned(x_dev, x_type) || misaligned(y_dev, y_type) || misaligned(bias_dev, FSCNN_F32) || misaligned(workspace_dev, FSCNN_F32) ||
+        x_dev == y_dev)
+        return FSCNN_ERR_UNSUPPORTED;
     int dev;
     const fscnn_status_t s = have_device(&dev);
     if (s != FSCNN_OK) return s;
     if (dev != q->device) return FSCNN_ERR_MISMATCH;
+    const long long need = q4_sums_bytes(q, x_type, M);
+    float *sums = need && workspace_dev && workspace_bytes >= need ? static_cast<float *>(workspace_dev) : nullptr;
     FSCNN_HIP(launch_linear_q4(q, x_dev, x_type, ldx, x_scale_dev, x_scale_cols, M, bias_dev, negative_slope == 1.0f ? 0 : act_code(negative_slope),
-                               y_dev, y_type, ldy, (hipStream_t)stream));
+                               y_dev, y_type, ldy, sums, (hipStream_t)stream));
     return FSCNN_OK;
+}
+
+long long fscnn_linear_q4_workspace(const fscnn_q4_t *q, fscnn_dtype_t x_type, int M)
+{
+    if (!live(q) || !type_bytes(x_type) || M < 0) return -1;
+    return q4_sums_bytes(q, x_type, M);
 }
 
 fscnn_status_t fscnn_rms_norm(const void *x_dev, fscnn_dtype_t x_type, long long ldx, const void *residual_dev, long long ldr,

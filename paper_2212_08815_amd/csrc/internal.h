@@ -222,8 +222,16 @@ hipError_t launch_q4_compress(const fscnn_q4 *q, const void *w, int type, long l
 hipError_t launch_q4_export(const fscnn_q4 *q, unsigned char *codes, void *scales, unsigned char *zeros, hipStream_t st);
 
 // ---- q4_linear.hip
+// Work-groups that may divide the columns of a call, if they have room for their sums: q4_sums_bytes(), or 0 where they do not divide them
+int q4_parts(const fscnn_q4 *q, int x_type, int M);
+inline long long q4_sums_bytes(const fscnn_q4 *q, int x_type, int M)
+{
+    const int parts = q4_parts(q, x_type, M);
+    return parts > 1 ? parts * (long long)M * q4_tiles(q->K) * 64 : 0;
+}
+// sums: that room, or NULL
 hipError_t launch_linear_q4(const fscnn_q4 *q, const void *x, int x_type, long long ldx, const float *x_scale, int x_scale_cols, int M,
-                            const float *bias, int act, void *y, int y_type, long long ldy, hipStream_t st);
+                            const float *bias, int act, void *y, int y_type, long long ldy, float *sums, hipStream_t st);
 
 // ---- rms_norm.hip
 constexpr int kNormMaxD = 65536;

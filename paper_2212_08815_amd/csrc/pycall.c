@@ -24,6 +24,7 @@ static struct {
     __typeof__(&fscnn_sparse_transpose) transpose;
     __typeof__(&fscnn_sparse_tensor_transpose) tensor_transpose;
     __typeof__(&fscnn_linear_q4) linear_q4;
+    __typeof__(&fscnn_linear_q4_workspace) linear_q4_workspace;
     __typeof__(&fscnn_rms_norm) rms_norm;
 } L;
 
@@ -31,7 +32,8 @@ static const char *const kNames[] = {
     "fscnn_conv2d_sparse_filter_ex", "fscnn_conv2d_sparse_filter_pool2x2", "fscnn_conv2d_sparse_filter_leaky",
     "fscnn_conv2d_sparse_filter_emit", "fscnn_conv2d_sparse_filter_emit_into", "fscnn_conv2d_sparse_input",
     "fscnn_conv2d_sparse_input_prepared", "fscnn_filter_compress", "fscnn_filter_info", "fscnn_input_compress",
-    "fscnn_input_info", "fscnn_sparse_transpose", "fscnn_sparse_tensor_transpose", "fscnn_linear_q4", "fscnn_rms_norm",
+    "fscnn_input_info", "fscnn_sparse_transpose", "fscnn_sparse_tensor_transpose", "fscnn_linear_q4",
+    "fscnn_linear_q4_workspace", "fscnn_rms_norm",
 };
 enum { kEntries = sizeof(kNames) / sizeof(kNames[0]) };
 _Static_assert(sizeof(L) == kEntries * sizeof(void *), "one name per entry point");
@@ -221,10 +223,10 @@ static PyObject *py_transpose(PyObject *self, PyObject *const *a, Py_ssize_t n)
     return PyLong_FromLong(st);
 }
 
-/* linear_q4(q, x, x_type, ldx, x_scale, x_scale_cols, M, C, bias, slope, y, y_type, ldy, stream) -> status */
+/* linear_q4(q, x, x_type, ldx, x_scale, x_scale_cols, M, C, bias, slope, y, y_type, ldy, workspace, workspace_bytes, stream) -> status */
 static PyObject *py_linear_q4(PyObject *self, PyObject *const *a, Py_ssize_t n)
 {
-    if (wrong_count(n, 14)) return NULL;
+    if (wrong_count(n, 16)) return NULL;
     int bad = 0, st = 0;
     void *q = getp(a[0], &bad), *x = getp(a[1], &bad);
     const int xt = geti(a[2], &bad);
@@ -236,9 +238,25 @@ static PyObject *py_linear_q4(PyObject *self, PyObject *const *a, Py_ssize_t n)
     void *y = getp(a[10], &bad);
     const int yt = geti(a[11], &bad);
     const long long ldy = getll(a[12], &bad);
-    void *s = getp(a[13], &bad);
-    CALL(L.linear_q4(q, x, xt, ldx, xs, cols, M, C, b, slope, y, yt, ldy, s));
+    void *w = getp(a[13], &bad);
+    const long long wb = getll(a[14], &bad);
+    void *s = getp(a[15], &bad);
+    CALL(L.linear_q4(q, x, xt, ldx, xs, cols, M, C, b, slope, y, yt, ldy, w, wb, s));
     return PyLong_FromLong(st);
+}
+
+/* linear_q4_workspace(q, x_type, M) -> bytes */
+static PyObject *py_linear_q4_workspace(PyObject *self, PyObject *const *a, Py_ssize_t n)
+{
+    if (wrong_count(n, 3)) return NULL;
+    int bad = 0;
+    void *q = getp(a[0], &bad);
+    const int xt = geti(a[1], &bad), M = geti(a[2], &bad);
+    if (bad || !L.conv_ex) {
+        if (!bad) PyErr_SetString(PyExc_RuntimeError, "bind() first");
+        return NULL;
+    }
+    return PyLong_FromLongLong(L.linear_q4_workspace(q, xt, M));
 }
 
 /* rms_norm(x, x_type, ldx, residual, ldr, residual_out, ldo, weight, weight_type, M, D, eps, y, y_type, ldy, scale, group, stream) -> status */
@@ -271,7 +289,7 @@ static PyMethodDef methods[] = {
     {"bind", py_bind, METH_O, NULL},
     FAST("conv", py_conv), FAST("emit", py_emit), FAST("conv_si", py_conv_si), FAST("conv_sip", py_conv_sip),
     FAST("compress", py_compress), FAST("transpose", py_transpose),
-    FAST("linear_q4", py_linear_q4), FAST("rms_norm", py_rms_norm),
+    FAST("linear_q4", py_linear_q4), FAST("linear_q4_workspace", py_linear_q4_workspace), FAST("rms_norm", py_rms_norm),
     {NULL, NULL, 0, NULL},
 };
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fscnn_call", NULL, -1, methods, NULL, NULL, NULL, NULL};

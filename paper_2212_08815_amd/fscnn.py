@@ -37,7 +37,7 @@ EXPORTS = [
     "fscnn_si_variant_count", "fscnn_conv2d_sparse_filter_leaky", "fscnn_sparse_transpose_noalloc",
     "fscnn_filter_prepare_ex", "fscnn_sf_band_choice", "fscnn_sf_contract_choice", "fscnn_sf_split_choice", "fscnn_sf_serves", "fscnn_si_contract_choice", "fscnn_si_split_choice", "fscnn_pool_trim",
     "fscnn_q4_compress", "fscnn_q4_import", "fscnn_q4_info", "fscnn_q4_export", "fscnn_q4_destroy",
-    "fscnn_linear_q4", "fscnn_rms_norm",
+    "fscnn_linear_q4", "fscnn_linear_q4_workspace", "fscnn_rms_norm",
 ]
 
 NCHW, N4 = 0, 1      # fscnn_layout_t
@@ -65,10 +65,11 @@ def lib():
         L.fscnn_sf_variant_count.restype = ctypes.c_int
         L.fscnn_sparse_transpose_workspace.restype = ctypes.c_longlong
         L.fscnn_sparse_transpose_workspace.argtypes = [ctypes.c_longlong, ctypes.c_longlong]
+        L.fscnn_linear_q4_workspace.restype = ctypes.c_longlong
         for name in EXPORTS:
             fn = getattr(L, name)
             if name not in ("fscnn_status_string", "fscnn_sf_variant_name", "fscnn_sf_variant_count",
-                            "fscnn_sparse_transpose_workspace"):
+                            "fscnn_sparse_transpose_workspace", "fscnn_linear_q4_workspace"):
                 fn.restype = ctypes.c_int
         _lib = L
     return _lib
@@ -769,8 +770,14 @@ def linear_q4(q, x, bias=None, relu=False, leaky=None, out=None, out_dtype=None,
         slope = leaky
     else:
         slope = 0.0 if relu else 1.0
-    st = (_nat or _native()).linear_q4(q.address, x.data_ptr(), _DTYPES[x.dtype], ldx, scale, cols, M, C, b, slope, out.data_ptr(), _DTYPES[want],
-                                       ldy, torch._C._cuda_getCurrentRawStream(dev))
+    native, h, xt = _nat or _native(), q.address, _DTYPES[x.dtype]
+    ws, need = None, 0
+    if xt == F32:                            # (the only type that wants scratch)
+        need = native.linear_q4_workspace(h, xt, M)
+        if need > 0:
+            ws = x.new_empty(need // 4)
+    st = native.linear_q4(h, x.data_ptr(), xt, ldx, scale, cols, M, C, b, slope, out.data_ptr(), _DTYPES[want], ldy, None if ws is None else ws.data_ptr(),
+                          need, torch._C._cuda_getCurrentRawStream(dev))
     if st != OK:
         raise FscnnError(st, "fscnn_linear_q4")
     return out

@@ -52,9 +52,10 @@ def test_weights(L):
 def test_linear(L):
     junk = (ctypes.c_ubyte * 512)()
     jp = ctypes.byref(junk)
-    lin = lambda q=jp, x=fake, M=1: L.fscnn_linear_q4(q, x, F32, ll(8), None, 1, M, 8, None, fl(1), ctypes.c_void_p(512), F32, ll(8), None)
+    lin = lambda q=jp, x=fake, M=1: L.fscnn_linear_q4(q, x, F32, ll(8), None, 1, M, 8, None, fl(1), ctypes.c_void_p(512), F32, ll(8), None, ll(0), None)
     assert lin(q=None) == lin(x=None) == NULL
     assert lin() == lin(M=0) == lin(M=-1) == HANDLE
+    assert L.fscnn_linear_q4_workspace(None, F32, 1) == L.fscnn_linear_q4_workspace(jp, F32, 1) == -1
 
 
 def test_norm(L):
@@ -98,7 +99,7 @@ def test_native_calls_count_and_read_their_arguments(L):
     m = fscnn._native()
     junk = (ctypes.c_ubyte * 512)()
     h = ctypes.addressof(junk)
-    args = [h, 256, F32, 8, None, 1, 1, 8, None, 1.0, 512, F32, 8, 0]
+    args = [h, 256, F32, 8, None, 1, 1, 8, None, 1.0, 512, F32, 8, None, 0, 0]
     assert m.linear_q4(*args) == HANDLE
     for i, v, err in ((3, "8", TypeError), (3, 1 << 70, OverflowError), (6, 1 << 31, OverflowError), (9, "x", TypeError), (2, None, TypeError)):
         with pytest.raises(err):
