@@ -228,6 +228,8 @@ __global__ void __launch_bounds__(WM * WN * WK * 64, XT == FSCNN_F32 ? 1 : 2) ti
     using T = Tile<XT>;
     constexpr bool kInt = XT == FSCNN_I8;
     constexpr int kRows = 32 * MT * WM, kSet = WM * WN * 64, kParts = X::kParts, kCh = T::kChunks, kGroups = 4 / STEPS;
+    constexpr int kAnyAlu = 6;                            // of sched_barrier: vector and scalar arithmetic may pass
+    constexpr int kSteps = kInt ? 4 : 8, kStepsOfGroup = kSteps / kGroups;   // products of a block, of a group
     constexpr int kPer = kRows * kCh / kSet;              // chunks a thread brings
     constexpr int kBuf = kRows * kCh * kParts;            // chunks of a buffer
     constexpr int kScales = GS ? 2 * kGroups * kRows / 4 : 0;
@@ -235,7 +237,9 @@ __global__ void __launch_bounds__(WM * WN * WK * 64, XT == FSCNN_F32 ? 1 : 2) ti
     constexpr int kChunksOfSet = 2 * kBuf + kScales;
     static_assert(kPer * kSet == kRows * kCh, "a whole number of chunks a thread");
     static_assert(!GS || kRows <= kSet, "a thread a row");
-    __shared__ u4v lds[kChunksOfSet * WK > kSums ? kChunksOfSet * WK : kSums];
+    constexpr int kPitch = 32 * NT * WN + 8, kArea = 32 * WM * kPitch;   // of outputs, in floats: rows 4 apart half of the banks apart
+    constexpr int kNeed = kSums * 4 > 2 * kArea ? kSums : (2 * kArea + 3) / 4;
+    __shared__ u4v lds[kChunksOfSet * WK > kNeed ? kChunksOfSet * WK : kNeed];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wk = wave / (WM * WN), in_set = wave % (WM * WN), half = lane >> 5, wm = in_set / WN, wn = in_set % WN;
     // panels of 8 tiles of x: work-groups that run together share both operands
@@ -244,14 +248,17 @@ __global__ void __launch_bounds__(WM * WN * WK * 64, XT == FSCNN_F32 ? 1 : 2) ti
     const int m0 = (panel * 8 + in % tall) * kRows, n0 = in / tall * (32 * NT * WN) + wn * (32 * NT);
     auto swizzle = [](int r) { return kCh == 16 ? r & 15 : r >> 1 & 7; };
 
-    const u4v *codes[NT];
-    const uint32_t *scales[NT];
+    // codes and scales: a base for the wave, which moves from block to block, and what a lane is away from it
+    const int first = (n0 >> 4) < a.tiles ? n0 >> 4 : a.tiles - 1;
+    const char *codes = reinterpret_cast<const char *>(a.codes) + ((long long)first * a.blocks + wk) * 1024;
+    const char *scales = reinterpret_cast<const char *>(a.scales) + ((long long)first * a.blocks + wk) * (kGroups * 64);
+    uint32_t code_at[NT], scale_at[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {            // (tiles past the last one repeat it: their outputs are not stored)
         int tile = (n0 + 32 * t + (lane & 31)) >> 4;
-        tile = tile < a.tiles ? tile : a.tiles - 1;
-        codes[t] = a.codes + (long long)tile * a.blocks * 64 + (lane & 15) + 32 * half;
-        scales[t] = a.scales + (long long)tile * a.blocks * (kGroups * 16) + (lane & 15);
+        tile = (tile < a.tiles ? tile : a.tiles - 1) - first;
+        code_at[t] = tile * a.blocks * 1024 + ((lane & 15) + 32 * half) * 16;
+        scale_at[t] = tile * a.blocks * (kGroups * 64) + (lane & 15) * 4;
     }
     const int live = a.M - m0 < kRows ? a.M - m0 : kRows;
     const char *x = a.x + m0 * a.ldx;
@@ -259,11 +266,8 @@ __global__ void __launch_bounds__(WM * WN * WK * 64, XT == FSCNN_F32 ? 1 : 2) ti
     float *const set_scales = reinterpret_cast<float *>(set + 2 * kBuf);
     const int slot = in_set * kPer * 64 + lane;           // of the thread's first chunk; the others follow 64 apart
     int from[DMA ? kPer : 1];
-    int4v rsrc = {};
     if constexpr (DMA) {
         // (rows that are not there are out of the descriptor's range and read as zeros)
-        const unsigned long long xa = (unsigned long long)x;
-        rsrc = int4v{(int)(uint32_t)xa, (int)(uint32_t)(xa >> 32), (int)((live - 1) * a.ldx + a.C * (16 / T::kChunk)), 0x00020000};
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
             const int at = slot + i * 64, r = at / kCh, c = at % kCh ^ swizzle(r);
@@ -301,9 +305,12 @@ __global__ void __launch_bounds__(WM * WN * WK * 64, XT == FSCNN_F32 ? 1 : 2) ti
     auto fetch = [&](int b, int buf) {
         if constexpr (DMA) {
             if ((b + 1) * kQ4Block <= a.C) {
+                const unsigned long long xa = (unsigned long long)x + (unsigned)b * (kCh * 16);
+                const int4v rsrc = {(int)(uint32_t)xa, (int)(uint32_t)(xa >> 32), (int)((live - 1) * a.ldx + a.C * (16 / T::kChunk)) - b * (kCh * 16), 0x00020000};
 #pragma unroll
-                for (int i = 0; i < kPer; ++i) lds_dma_dwordx4(rsrc, lds0 + buf * (kBuf * 16) + i * 1024, from[i] + b * (kCh * 16));
+                for (int i = 0; i < kPer; ++i) lds_dma_dwordx4(rsrc, lds0 + buf * (kBuf * 16) + i * 1024, from[i]);
             } else {
+#pragma unroll 1
                 for (int i = 0; i < kPer; ++i) put_chunk(buf, i, load_chunk(b, i));
             }
         } else {
@@ -321,10 +328,12 @@ __global__ void __launch_bounds__(WM * WN * WK * 64, XT == FSCNN_F32 ? 1 : 2) ti
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
 #pragma unroll
-            for (int e = 0; e < 2; ++e) next[t][e] = codes[t][(long long)b * 64 + 16 * e];
+            for (int e = 0; e < 2; ++e) next[t][e] = *reinterpret_cast<const u4v *>(codes + (code_at[t] + 256 * e));
 #pragma unroll
-            for (int g = 0; g < kGroups; ++g) word[t][g] = scales[t][((long long)b * kGroups + g) * 16];
+            for (int g = 0; g < kGroups; ++g) word[t][g] = *reinterpret_cast<const uint32_t *>(scales + (scale_at[t] + 64 * g));
         }
+        codes += WK * 1024;
+        scales += WK * (kGroups * 64);
     };
     auto commit = [&](int buf) {
         if constexpr (!DMA) {
@@ -349,8 +358,6 @@ __global__ void __launch_bounds__(WM * WN * WK * 64, XT == FSCNN_F32 ? 1 : 2) ti
     for (int turn = 0; turn < turns; ++turn) {
         const int b = turn * WK + wk, buf = turn & 1;
         wait_vmcnt<0>();                      // the block is in LDS, its codes in registers
-        __syncthreads();
-        if (b >= a.blocks) continue;          // (the last turn of some sets)
         u4v now[NT][2];
         uint32_t sz[NT][kGroups];
 #pragma unroll
@@ -360,62 +367,68 @@ __global__ void __launch_bounds__(WM * WN * WK * 64, XT == FSCNN_F32 ? 1 : 2) ti
 #pragma unroll
             for (int g = 0; g < kGroups; ++g) sz[t][g] = word[t][g];
         }
-        const bool more = b + WK < a.blocks;
-        if (more) fetch(b + WK, buf ^ 1);
-        const u4v *from_lds = set + buf * kBuf + row0 * kCh;
+        // step st of the block: the weights' operand
+        auto decode = [&](int st, u4v *w) {
 #pragma unroll
-        for (int g = 0; g < kGroups; ++g) {
-            typename T::Acc acc[MT][NT] = {};
-            typename X::Zero z[NT];
-#pragma unroll
-            for (int t = 0; t < NT; ++t) z[t] = X::zero(sz[t][g]);
-#pragma unroll
-            for (int s = g * STEPS; s < (g + 1) * STEPS; ++s) {
+            for (int t = 0; t < NT; ++t) {
+                const typename X::Zero z = X::zero(sz[t][st / kStepsOfGroup]);
                 if constexpr (kInt) {
-                    u4v op[MT];
-#pragma unroll
-                    for (int u = 0; u < MT; ++u) op[u] = from_lds[u * 32 * kCh + ((2 * s + half) ^ swizzle(row0))];
-#pragma unroll
-                    for (int t = 0; t < NT; ++t) {
-                        const u2v w0 = X::weights(now[t][0][s], z[t]), w1 = X::weights(now[t][1][s], z[t]);
-#pragma unroll
-                        for (int u = 0; u < MT; ++u) acc[u][t] = T::mfma(op[u], u4v{w0[0], w0[1], w1[0], w1[1]}, acc[u][t]);
-                    }
+                    const u2v w0 = X::weights(now[t][0][st], z), w1 = X::weights(now[t][1][st], z);
+                    w[t] = u4v{w0[0], w0[1], w1[0], w1[1]};
                 } else {
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        u4v w[NT];
-#pragma unroll
-                        for (int t = 0; t < NT; ++t) w[t] = X::weights(now[t][e][s], z[t]);
-#pragma unroll
-                        for (int p = 0; p < kParts; ++p)
-#pragma unroll
-                            for (int u = 0; u < MT; ++u) {
-                                const u4v op = from_lds[p * kRows * kCh + u * 32 * kCh + ((4 * s + 2 * half + e) ^ swizzle(row0))];
-#pragma unroll
-                                for (int t = 0; t < NT; ++t) acc[u][t] = T::mfma(op, w[t], acc[u][t]);
-                            }
-                    }
+                    w[t] = X::weights(now[t][st & 1][st >> 1], z);
                 }
             }
+        };
+        const u4v *from_lds = set + buf * kBuf + row0 * kCh;
+        // part p of the rows of x at that step
+        auto read = [&](int st, int p, u4v *op) {
+            const int chunk = kInt ? 2 * st + half : 4 * (st >> 1) + 2 * half + (st & 1);
+#pragma unroll
+            for (int u = 0; u < MT; ++u) op[u] = from_lds[p * kRows * kCh + u * 32 * kCh + (chunk ^ swizzle(row0))];
+        };
+        u4v op[2][MT], w[2][NT];
+        decode(0, w[0]);
+        __syncthreads();
+        if (b >= a.blocks) continue;          // (the last turn of some sets)
+        const bool more = b + WK < a.blocks;
+        if (more) fetch(b + WK, buf ^ 1);
+        read(0, 0, op[0]);
+        typename T::Acc acc[MT][NT] = {};
+        // one part of one step after the other; what the next one needs is read and made beside the products
+#pragma unroll
+        for (int i = 0; i < kSteps * kParts; ++i) {
+            const int st = i / kParts, p = i % kParts;
+            const bool last = i + 1 == kSteps * kParts;
+            if (!last) read((i + 1) / kParts, (i + 1) % kParts, op[(i + 1) & 1]);
+            __builtin_amdgcn_sched_barrier(kAnyAlu);   // (else the reads sink to their uses, to save registers)
+#pragma unroll
+            for (int u = 0; u < MT; ++u)
+#pragma unroll
+                for (int t = 0; t < NT; ++t) acc[u][t] = T::mfma(op[i & 1][u], w[st & 1][t], acc[u][t]);
+            if (!last && p == kParts - 1) decode(st + 1, w[(st + 1) & 1]);
+            __builtin_amdgcn_sched_barrier(kAnyAlu);
+            if (p != kParts - 1 || (st + 1) % kStepsOfGroup) continue;
             // the group's end
+            const int g = st / kStepsOfGroup;
 #pragma unroll
             for (int u = 0; u < MT; ++u) {
                 q4f4 xs[4];
                 if constexpr (GS) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        xs[i] = *reinterpret_cast<const q4f4 *>(set_scales + (buf * kGroups + g) * kRows + wm * (32 * MT) + u * 32 + 8 * i + 4 * half);
+                    for (int j = 0; j < 4; ++j)
+                        xs[j] = *reinterpret_cast<const q4f4 *>(set_scales + (buf * kGroups + g) * kRows + wm * (32 * MT) + u * 32 + 8 * j + 4 * half);
                 }
 #pragma unroll
                 for (int t = 0; t < NT; ++t) {
                     const float f = __builtin_bit_cast(float, sz[t][g] & ~15u);
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        float v = (float)acc[u][t][i];
-                        if constexpr (GS) v *= xs[i >> 2][i & 3];
-                        total[u][t][i] = __builtin_fmaf(f, v, total[u][t][i]);
+                    for (int j = 0; j < 16; ++j) {
+                        float v = (float)acc[u][t][j];
+                        if constexpr (GS) v *= xs[j >> 2][j & 3];
+                        total[u][t][j] = __builtin_fmaf(f, v, total[u][t][j]);
                     }
+                    acc[u][t] = typename T::Acc{};
                 }
             }
             // (a second group's sums at the same time would not fit the registers)
@@ -437,28 +450,58 @@ __global__ void __launch_bounds__(WM * WN * WK * 64, XT == FSCNN_F32 ? 1 : 2) ti
                 out[((wk - 1) * MT * NT * 4 + e) * kSet + mine] = q4f4{f[e % 4 * 4], f[e % 4 * 4 + 1], f[e % 4 * 4 + 2], f[e % 4 * 4 + 3]};
             }
         __syncthreads();
-        if (wk > 0) return;
+        if (wk == 0)
 #pragma unroll
-        for (int e = 0; e < MT * NT * 4; ++e)
+            for (int e = 0; e < MT * NT * 4; ++e)
 #pragma unroll
-            for (int k = 0; k < WK - 1; ++k) {
-                const q4f4 f = out[(k * MT * NT * 4 + e) * kSet + mine];
+                for (int k = 0; k < WK - 1; ++k) {
+                    const q4f4 f = out[(k * MT * NT * 4 + e) * kSet + mine];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) total[e / 4 / NT][e / 4 % NT][e % 4 * 4 + i] += f[i];
-            }
+                    for (int i = 0; i < 4; ++i) total[e / 4 / NT][e / 4 % NT][e % 4 * 4 + i] += f[i];
+                }
     }
+    // 32 rows of every wave after the other by way of LDS, so that a lane stores 16 bytes of a row of y
+    float *const area = reinterpret_cast<float *>(lds);
+    const int cols0 = n0 - wn * (32 * NT);
+    const auto put = [&](int u) {
+        if (wk == 0)
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        const int k = n0 + 32 * t + (lane & 31);
-        if (k >= a.K) continue;
-        const float bias = a.bias ? a.bias[k] : 0.0f;
+            for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int u = 0; u < MT; ++u)
+                for (int i = 0; i < 16; ++i)
+                    area[(u & 1) * kArea + (wm * 32 + 8 * (i >> 2) + 4 * half + (i & 3)) * kPitch + wn * (32 * NT) + t * 32 + (lane & 31)] = total[u][t][i];
+    };
+    const auto store = [&](int u, auto type) {
+        using E = typename Elem<decltype(type)::value>::type;
+        constexpr int kV = 16 / (int)sizeof(E), kRow = 32 * NT * WN / kV;   // outputs of a thread; threads of a row
+        for (int at = threadIdx.x; at < 32 * WM * kRow; at += kSet * WK) {
+            const int r = at / kRow, c = at % kRow * kV, m = m0 + (r >> 5) * (32 * MT) + u * 32 + (r & 31), k = cols0 + c;
+            if (m >= a.M || k >= a.K) continue;
+            const float *f = area + (u & 1) * kArea + r * kPitch + c;
+            const float xs = kInt && !GS ? a.x_scale[m] : 1.0f;
+            E e[kV];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int m = m0 + wm * (32 * MT) + u * 32 + 8 * (i >> 2) + 4 * half + (i & 3);
-                if (m < a.M) store_output(a, m, k, kInt && !GS ? total[u][t][i] * a.x_scale[m] : total[u][t][i], bias);
+            for (int j = 0; j < kV; ++j) {
+                float v = f[j];
+                if (kInt && !GS) v *= xs;
+                e[j] = (E)act_apply(v + (a.bias && k + j < a.K ? a.bias[k + j] : 0.0f), a.act);
             }
+            E *y = static_cast<E *>(a.y) + (m * a.ldy + k);
+            if (k + kV <= a.K) __builtin_memcpy(y, e, 16);
+            else
+#pragma unroll
+                for (int j = 0; j < kV; ++j)
+                    if (k + j < a.K) y[j] = e[j];
+        }
+    };
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < MT; ++u) {            // (two areas: a barrier each)
+        put(u);
+        __syncthreads();
+        if (a.y_type == FSCNN_F32) store(u, std::integral_constant<int, FSCNN_F32>{});
+        else if (a.y_type == FSCNN_F16) store(u, std::integral_constant<int, FSCNN_F16>{});
+        else store(u, std::integral_constant<int, FSCNN_BF16>{});
     }
 }
 
