@@ -6,13 +6,13 @@ namespace fscnn {
 template <> hipError_t launch_q4_type<FSCNN_F32>(const Q4Args &a, int parts, hipStream_t st)
 {
     constexpr int XT = FSCNN_F32;
-    if (parts > 1 || a.M > 16) {
-        if (a.M <= 16) return launch_rows<XT, 4, 1, 8>(a, parts, st);
-        if (a.M <= 32) return launch_rows<XT, 4, 2, 8>(a, parts, st);
-        if (a.M <= 64) return launch_rows<XT, 2, 4, 4>(a, parts, st);
-        return launch_tiles<XT, 2, 2, 1, 4, 1>(a, st);
+    // every row's three parts in one operand; else a wave's own parts (few rows, little work) or a tile's, made once for 256 rows of weights
+    switch (f32_choice(a.tiles, a.blocks, a.M, parts).kernel) {
+        case F32Choice::kStaged: return a.blocks >= 64 && a.tiles <= 256 ? launch_staged<XT, 1, 16>(a, st) : launch_staged<XT, 1, 8>(a, st);
+        case F32Choice::kRows: return launch_rows<XT, 1, 1, 8>(a, st);
+        case F32Choice::kTile32: return launch_tiles<XT, 1, 1, 1, 8, 1, false, false>(a, parts, st);
+        default: return launch_tiles<XT, 2, 1, 1, 8, 1, false, false>(a, parts, st);
     }
-    return launch_rows<XT, 1, 1, 16>(a, 1, st);
 }
 
 }  // namespace fscnn

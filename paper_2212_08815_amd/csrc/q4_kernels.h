@@ -24,11 +24,37 @@ struct Q4Args {
     const char *x;
     const float *x_scale, *bias;
     void *y;
-    float *sums;                              // rows_kernel: [gridDim.z][M][16 tiles], where the blocks are divided
+    float *sums;                              // tile_kernel: [gridDim.y][M][16 tiles], where work-groups divide the blocks
     long long ldx, ldy;                       // ldx in bytes
     int K, C, M, blocks, tiles, steps, y_type, x_cols, act;   // steps: of 32 columns a group
     int mt, nt;                               // tile_kernel: tiles of the launch
 };
+
+// How 32-bit floats are served: kernel, and work-groups that divide the columns, at most `most` of them
+struct F32Choice {
+    enum Kernel { kStaged, kRows, kTile32, kTile64 } kernel;
+    int parts;
+};
+inline F32Choice f32_choice(long long tiles, int blocks, int M, int most)
+{
+    // (25088 -> 4096, one row: 14.1 us staged, 30 with a wave's own parts)
+    if (M * XOp<FSCNN_F32>::kParts <= 16) return {F32Choice::kStaged, 1};
+    // times of launches as TileCost has them; divided columns cost a launch and the sums' way to memory and back
+    const double wide = (double)((tiles + 15) / 16), sums = 1.28e-4 * M * tiles / 3;   // work-groups of a part of 32 or 64 rows; us a part
+    F32Choice best = {F32Choice::kTile32, 1};
+    double us = 1e30;
+    for (int rows = 32; rows <= 64; rows *= 2)
+        for (int p = 1; p <= most && p <= 16 && blocks / p >= 4; p *= 2) {
+            const double n = __builtin_ceil(wide * ((M + rows - 1) / rows) * p / 256);
+            const double t = 4 + n * ((blocks + p - 1) / p) * (rows == 32 ? 1.45 : 2.65) + (p > 1 ? 2.5 + p * sums : 0);
+            if (t < us) {
+                us = t;
+                best = {rows == 32 ? F32Choice::kTile32 : F32Choice::kTile64, p};
+            }
+        }
+    if (M <= 16 && 4 + __builtin_ceil(tiles / 256.0) * (blocks / 32.0) * (4 + 0.3 * M) < us) return {F32Choice::kRows, 1};
+    return best;
+}
 
 namespace {
 
@@ -77,28 +103,28 @@ template <int XT, int NT, int MT, int W, int STEPS> __global__ void __launch_bou
 #pragma unroll
         for (int u = 0; u < MT; ++u) raw[s][u] = load_columns<XT, decltype(tail)::value>(rows[u], b * kQ4Block + s * 32 + quarter * 8, a.C);
     };
-    // block b; its loads are done or on their way, those of block `then` are issued here (then < 0: none)
-    auto block = [&](int b, int then, const Weights &v, Weights &next) {
-        if (then >= 0) load_weights(then, next);
+    // block b; its loads are done or on their way, those of block `then` are issued here if there is one
+    auto block = [&](int b, int then, const Weights &v, Weights &next, auto has) {
+        if constexpr (decltype(has)::value) load_weights(then, next);
         typename X::Acc acc[NT][MT] = {}, sum[MT] = {};
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
             typename X::Op op[MT][X::kParts];
 #pragma unroll
             for (int u = 0; u < MT; ++u) X::parts(raw[s][u], op[u]);
-            if (then >= 0) load_x(then, s, std::false_type{});
+            if constexpr (decltype(has)::value) load_x(then, s, std::false_type{});
+            typename X::Op q[NT];
 #pragma unroll
-            for (int u = 0; u < MT; ++u)
+            for (int t = 0; t < NT; ++t) q[t] = X::codes(v.w[t][s]);
+            // (parts outermost: products that follow each other add to different sums)
 #pragma unroll
-                for (int p = 0; p < X::kParts; ++p) sum[u] = X::mfma(op[u][p], X::ones(), sum[u]);
+            for (int p = 0; p < X::kParts; ++p)
 #pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                const typename X::Op q = X::codes(v.w[t][s]);
+                for (int u = 0; u < MT; ++u) {
+                    sum[u] = X::mfma(op[u][p], X::ones(), sum[u]);
 #pragma unroll
-                for (int u = 0; u < MT; ++u)
-#pragma unroll
-                    for (int p = 0; p < X::kParts; ++p) acc[t][u] = X::mfma(op[u][p], q, acc[t][u]);
-            }
+                    for (int t = 0; t < NT; ++t) acc[t][u] = X::mfma(op[u][p], q[t], acc[t][u]);
+                }
             if ((s + 1) % STEPS == 0) {       // the group's end
                 const int g = b * kGroups + s / STEPS;
                 q4f4 xs[MT];
@@ -138,33 +164,25 @@ template <int XT, int NT, int MT, int W, int STEPS> __global__ void __launch_bou
             }
         }
     };
-    // this work-group's blocks: b0 up to b1, the last one of all perhaps a part of one
-    const int b0 = (int)((long long)a.blocks * blockIdx.z / gridDim.z), b1 = (int)((long long)a.blocks * (blockIdx.z + 1) / gridDim.z);
-    const int whole = a.C / kQ4Block < b1 ? a.C / kQ4Block : b1;
-    Weights v[2];
-    int b = b0 + wave;
+    const int whole = a.C / kQ4Block;         // (the last block may be a part of one)
+    Weights v, next;
+    int b = wave;
     if (b < whole) {
-        load_weights(b, v[0]);
+        load_weights(b, v);
 #pragma unroll
         for (int s = 0; s < 4; ++s) load_x(b, s, std::false_type{});
-        for (; b + 2 * W < whole; b += 2 * W) {
-            block(b, b + W, v[0], v[1]);
-            block(b + W, b + 2 * W, v[1], v[0]);
+        for (; b + W < whole; b += W) {
+            block(b, b + W, v, next, std::true_type{});
+            v = next;
         }
-        if (b + W < whole) {
-            block(b, b + W, v[0], v[1]);
-            block(b + W, -1, v[1], v[0]);
-            b += 2 * W;
-        } else {
-            block(b, -1, v[0], v[1]);
-            b += W;
-        }
+        block(b, 0, v, next, std::false_type{});
+        b += W;
     }
-    if (b < b1) {
-        load_weights(b, v[0]);
+    if (b < a.blocks) {
+        load_weights(b, v);
 #pragma unroll
         for (int s = 0; s < 4; ++s) load_x(b, s, std::true_type{});
-        block(b, -1, v[0], v[1]);
+        block(b, 0, v, next, std::false_type{});
     }
 
     __shared__ q4f4 sums[W][NT * MT][64];
@@ -178,17 +196,149 @@ template <int XT, int NT, int MT, int W, int STEPS> __global__ void __launch_bou
 #pragma unroll
         for (int i = 1; i < W; ++i) f += sums[i][e][lane];
         const int m = m0 + e % MT * 16 + 4 * quarter, k = (tile0 + e / MT) * 16 + col16;
-        if (gridDim.z > 1) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (m + i < a.M && k < a.K) a.sums[((long long)blockIdx.z * a.M + m + i) * (a.tiles * 16LL) + k] = f[i];
-            continue;
-        }
         if (k >= a.K) continue;
         const float bias = a.bias ? a.bias[k] : 0.0f;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             if (m + i < a.M) store_output(a, m + i, k, kInt && a.x_cols == 1 ? f[i] * a.x_scale[m + i] : f[i], bias);
+    }
+}
+
+// Few rows of x: all of them, each of their parts, are the 16 rows of one operand, so that a row of x costs a third of a product and not three.  The
+// operand is made once for a work-group: `cols` columns at a time lie in LDS, rows 16 bytes more than that apart (a multiple of 256 bytes:
+// the 16 rows of a chunk are in all banks).  NT tiles of weights, W waves that divide the blocks; their sums are added as rows_kernel adds them.
+template <int XT> using RowOp = XOp<XT == FSCNN_F32 ? FSCNN_BF16 : XT>;
+template <int XT, int NT, int W, int STEPS> __global__ void __launch_bounds__(W * 64) staged_kernel(const Q4Args a, int cols)
+{
+    using X = XOp<XT>;
+    using R = RowOp<XT>;
+    constexpr bool kInt = XT == FSCNN_I8;
+    constexpr int kGroups = 4 / STEPS, kBytes = kInt ? 1 : 2, kParts = X::kParts;
+    extern __shared__ __align__(256) char lds[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int col16 = lane & 15, quarter = lane >> 4;
+    const int tile0 = blockIdx.x * NT, pitch = cols * kBytes + 16;
+    const u4v *codes[NT];
+    const uint32_t *scales[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {            // (tiles past the last one repeat it: their outputs are not stored)
+        const long long tile = tile0 + t < a.tiles ? tile0 + t : a.tiles - 1;
+        codes[t] = a.codes + tile * a.blocks * 64 + lane;
+        scales[t] = a.scales + tile * a.blocks * (kGroups * 16) + col16;
+    }
+    struct Weights {
+        u4v w[NT];
+        uint32_t sz[NT][kGroups];
+    };
+    auto load_weights = [&](int b, Weights &v) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) v.w[t] = codes[t][(long long)b * 64];
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int g = 0; g < kGroups; ++g) v.sz[t][g] = scales[t][((long long)b * kGroups + g) * 16];
+    };
+    const int rows = a.M * kParts;            // at most 16; the operand's others repeat the last one
+    const char *mine = lds + (col16 < rows ? col16 : rows - 1) * pitch + quarter * (8 * kBytes);
+    q4f4 total[NT] = {};
+    // Codes are two blocks ahead, in three slots.  (Every step loads, past the last block that one again: the waits count loads.)
+    Weights v[3];
+    auto block_at = [&](int i) { return i < a.blocks ? i : a.blocks - 1; };
+    int b = wave;
+    for (int c0 = 0; c0 < a.blocks * kQ4Block; c0 += cols) {
+        load_weights(block_at(b), v[0]);
+        load_weights(block_at(b + W), v[1]);
+        if (c0) __syncthreads();
+        const int end = a.blocks * kQ4Block - c0 < cols ? a.blocks * kQ4Block - c0 : cols;
+        const int inside = a.C - c0 < end ? (a.C - c0) & ~7 : end;   // columns in whole chunks of 8; then those that end in C, and zeros
+        auto put = [&](int m, int c, const typename X::Raw &raw) {
+            typename X::Op op[kParts];
+            X::parts(raw, op);
+#pragma unroll
+            for (int p = 0; p < kParts; ++p) *reinterpret_cast<typename X::Op *>(lds + (m * kParts + p) * pitch + c * kBytes) = op[p];
+        };
+        const int chunks = inside / 8, each = chunks * a.M;
+        for (int i = threadIdx.x; i < each; i += W * 64 * 4) {       // four loads on their way
+            typename X::Raw raw[4];
+            int m[4], c[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int at = i + j * (W * 64) < each ? i + j * (W * 64) : i;
+                m[j] = at / chunks;
+                c[j] = (at - m[j] * chunks) * 8;
+                raw[j] = load_columns<XT, false>(a.x + m[j] * a.ldx, c0 + c[j], a.C);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (j == 0 || i + j * (W * 64) < each) put(m[j], c[j], raw[j]);
+        }
+        for (int i = threadIdx.x; i < (end - inside) / 8 * a.M; i += W * 64) {
+            const int m = i % a.M, c = inside + i / a.M * 8;
+            put(m, c, load_columns<XT, true>(a.x + m * a.ldx, c0 + c, a.C));
+        }
+        __syncthreads();
+        auto block = [&](const Weights &now, Weights &after) {
+            load_weights(block_at(b + 2 * W), after);
+            q4f4 xs[kInt ? kGroups : 1];
+            if constexpr (kInt) {
+#pragma unroll
+                for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        xs[g][i] = 1.0f;
+                        const int m = 4 * quarter + i, group = b * kGroups + g;
+                        if (a.x_cols > 1 && m < a.M && group < a.x_cols) xs[g][i] = a.x_scale[(long long)m * a.x_cols + group];
+                    }
+            }
+            const char *from = mine + (b * kQ4Block - c0) * kBytes;
+            typename R::Op op[4];
+#pragma unroll
+            for (int s = 0; s < 4; ++s) op[s] = *reinterpret_cast<const typename R::Op *>(from + s * (32 * kBytes));
+            typename R::Acc acc[NT] = {}, sum = {};
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                sum = R::mfma(op[s], R::ones(), sum);
+#pragma unroll
+                for (int t = 0; t < NT; ++t) acc[t] = R::mfma(op[s], R::codes(now.w[t][s]), acc[t]);
+                if ((s + 1) % STEPS == 0) {
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) {
+                        const uint32_t sz = now.sz[t][s / STEPS];
+                        const float f = __builtin_bit_cast(float, sz & ~15u), z = -(float)(sz & 15);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            float w;
+                            if constexpr (kInt) w = (float)(acc[t][i] - (int)(sz & 15) * sum[i]) * xs[s / STEPS][i];
+                            else w = __builtin_fmaf(z, sum[i], acc[t][i]);
+                            total[t][i] = __builtin_fmaf(f, w, total[t][i]);
+                        }
+                        acc[t] = typename R::Acc{};
+                    }
+                    sum = typename R::Acc{};
+                }
+            }
+            b += W;
+            return b * kQ4Block < c0 + end;
+        };
+        if (b * kQ4Block < c0 + end)
+            while (block(v[0], v[2]) && block(v[1], v[0]) && block(v[2], v[1])) {}
+    }
+    __syncthreads();
+    float *const sums = reinterpret_cast<float *>(lds);   // [W][NT][64 lanes][4]
+#pragma unroll
+    for (int t = 0; t < NT; ++t) *reinterpret_cast<q4f4 *>(sums + ((wave * NT + t) * 64 + lane) * 4) = total[t];
+    __syncthreads();
+    for (int e = threadIdx.x; e < a.M * (16 * NT); e += W * 64) {
+        const int m = e / (16 * NT), t = e / 16 % NT, k = (tile0 + t) * 16 + (e & 15);
+        float f = 0.0f;
+#pragma unroll
+        for (int p = 0; p < kParts; ++p) {
+            const int row = m * kParts + p, at = ((row >> 2) * 16 + (e & 15)) * 4 + (row & 3);
+#pragma unroll
+            for (int w = 0; w < W; ++w) f += sums[(w * NT + t) * 256 + at];
+        }
+        if (k >= a.K) continue;
+        store_output(a, m, k, kInt && a.x_cols == 1 ? f * a.x_scale[m] : f, a.bias ? a.bias[k] : 0.0f);
     }
 }
 
@@ -250,8 +400,10 @@ __global__ void __launch_bounds__(WM * WN * WK * 64, XT == FSCNN_F32 ? 1 : 2) ti
 
     // codes and scales: a base for the wave, which moves from block to block, and what a lane is away from it
     const int first = (n0 >> 4) < a.tiles ? n0 >> 4 : a.tiles - 1;
-    const char *codes = reinterpret_cast<const char *>(a.codes) + ((long long)first * a.blocks + wk) * 1024;
-    const char *scales = reinterpret_cast<const char *>(a.scales) + ((long long)first * a.blocks + wk) * (kGroups * 64);
+    // (this work-group's blocks: b0 up to b1)
+    const int b0 = (int)((long long)a.blocks * blockIdx.y / gridDim.y), b1 = (int)((long long)a.blocks * (blockIdx.y + 1) / gridDim.y);
+    const char *codes = reinterpret_cast<const char *>(a.codes) + ((long long)first * a.blocks + b0 + wk) * 1024;
+    const char *scales = reinterpret_cast<const char *>(a.scales) + ((long long)first * a.blocks + b0 + wk) * (kGroups * 64);
     uint32_t code_at[NT], scale_at[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {            // (tiles past the last one repeat it: their outputs are not stored)
@@ -275,16 +427,15 @@ __global__ void __launch_bounds__(WM * WN * WK * 64, XT == FSCNN_F32 ? 1 : 2) ti
         }
     }
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) u4v *)set + in_set * kPer * 1024;
-    // a block of the rows of x by way of registers
+    // a block of the rows of x by way of registers (rows that are not there repeat the last one: their outputs are not stored)
     struct Chunk { typename X::Raw r[kInt ? 2 : 1]; };
-    auto load_chunk = [&](int b, int i) {
+    auto load_chunk = [&](int b, int i, auto tail) {
+        constexpr bool kTail = decltype(tail)::value;
         const int at = slot + i * 64, r = at / kCh, c = at % kCh ^ swizzle(r), col = b * kQ4Block + c * T::kChunk;
-        Chunk v = {};
-        if (r < live) {
-            const char *row = x + r * a.ldx;
-            v.r[0] = load_columns<XT, true>(row, col, a.C);
-            if constexpr (kInt) v.r[1] = load_columns<XT, true>(row, col + 8, a.C);
-        }
+        const char *row = x + (r < live ? r : live - 1) * a.ldx;
+        Chunk v;
+        v.r[0] = load_columns<XT, kTail>(row, col, a.C);
+        if constexpr (kInt) v.r[1] = load_columns<XT, kTail>(row, col + 8, a.C);
         return v;
     };
     auto put_chunk = [&](int buf, int i, const Chunk &v) {
@@ -299,8 +450,21 @@ __global__ void __launch_bounds__(WM * WN * WK * 64, XT == FSCNN_F32 ? 1 : 2) ti
     };
     Chunk raw[DMA ? 1 : kPer];
     float xs_next[GS ? kGroups : 1];
-    u4v next[NT][2];
-    uint32_t word[NT][kGroups];
+    struct Weights {
+        u4v w[NT][2];
+        uint32_t sz[NT][kGroups];
+    } now, next;
+    auto load_weights = [&](Weights &v) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) v.w[t][e] = *reinterpret_cast<const u4v *>(codes + (code_at[t] + 256 * e));
+#pragma unroll
+            for (int g = 0; g < kGroups; ++g) v.sz[t][g] = *reinterpret_cast<const uint32_t *>(scales + (scale_at[t] + 64 * g));
+        }
+        codes += WK * 1024;
+        scales += WK * (kGroups * 64);
+    };
     // brings block b on its way to buffer `buf`; what goes through registers is put there by commit()
     auto fetch = [&](int b, int buf) {
         if constexpr (DMA) {
@@ -311,11 +475,16 @@ __global__ void __launch_bounds__(WM * WN * WK * 64, XT == FSCNN_F32 ? 1 : 2) ti
                 for (int i = 0; i < kPer; ++i) lds_dma_dwordx4(rsrc, lds0 + buf * (kBuf * 16) + i * 1024, from[i]);
             } else {
 #pragma unroll 1
-                for (int i = 0; i < kPer; ++i) put_chunk(buf, i, load_chunk(b, i));
+                for (int i = 0; i < kPer; ++i) put_chunk(buf, i, load_chunk(b, i, std::true_type{}));
             }
         } else {
+            if ((b + 1) * kQ4Block <= a.C) {
 #pragma unroll
-            for (int i = 0; i < kPer; ++i) raw[i] = load_chunk(b, i);
+                for (int i = 0; i < kPer; ++i) raw[i] = load_chunk(b, i, std::false_type{});
+            } else {
+#pragma unroll
+                for (int i = 0; i < kPer; ++i) raw[i] = load_chunk(b, i, std::true_type{});
+            }
         }
         if constexpr (GS) {
             const int r = in_set * 64 + lane;
@@ -325,15 +494,6 @@ __global__ void __launch_bounds__(WM * WN * WK * 64, XT == FSCNN_F32 ? 1 : 2) ti
                 xs_next[g] = r < live && group < a.x_cols ? a.x_scale[(long long)(m0 + r) * a.x_cols + group] : 0.0f;
             }
         }
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-#pragma unroll
-            for (int e = 0; e < 2; ++e) next[t][e] = *reinterpret_cast<const u4v *>(codes + (code_at[t] + 256 * e));
-#pragma unroll
-            for (int g = 0; g < kGroups; ++g) word[t][g] = *reinterpret_cast<const uint32_t *>(scales + (scale_at[t] + 64 * g));
-        }
-        codes += WK * 1024;
-        scales += WK * (kGroups * 64);
     };
     auto commit = [&](int buf) {
         if constexpr (!DMA) {
@@ -349,34 +509,27 @@ __global__ void __launch_bounds__(WM * WN * WK * 64, XT == FSCNN_F32 ? 1 : 2) ti
     };
     q4f16 total[MT][NT] = {};
     const int row0 = wm * (32 * MT) + (lane & 31);
-    const int turns = (a.blocks + WK - 1) / WK;
+    const int turns = (b1 - b0 + WK - 1) / WK;
 
-    if (wk < a.blocks) {
-        fetch(wk, 0);
+    if (b0 + wk < b1) {
+        load_weights(next);
+        fetch(b0 + wk, 0);
         commit(0);
     }
     for (int turn = 0; turn < turns; ++turn) {
-        const int b = turn * WK + wk, buf = turn & 1;
+        const int b = b0 + turn * WK + wk, buf = turn & 1;
         wait_vmcnt<0>();                      // the block is in LDS, its codes in registers
-        u4v now[NT][2];
-        uint32_t sz[NT][kGroups];
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            now[t][0] = next[t][0];
-            now[t][1] = next[t][1];
-#pragma unroll
-            for (int g = 0; g < kGroups; ++g) sz[t][g] = word[t][g];
-        }
+        now = next;
         // step st of the block: the weights' operand
         auto decode = [&](int st, u4v *w) {
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
-                const typename X::Zero z = X::zero(sz[t][st / kStepsOfGroup]);
+                const typename X::Zero z = X::zero(now.sz[t][st / kStepsOfGroup]);
                 if constexpr (kInt) {
-                    const u2v w0 = X::weights(now[t][0][st], z), w1 = X::weights(now[t][1][st], z);
+                    const u2v w0 = X::weights(now.w[t][0][st], z), w1 = X::weights(now.w[t][1][st], z);
                     w[t] = u4v{w0[0], w0[1], w1[0], w1[1]};
                 } else {
-                    w[t] = X::weights(now[t][st & 1][st >> 1], z);
+                    w[t] = X::weights(now.w[t][st & 1][st >> 1], z);
                 }
             }
         };
@@ -389,10 +542,13 @@ __global__ void __launch_bounds__(WM * WN * WK * 64, XT == FSCNN_F32 ? 1 : 2) ti
         };
         u4v op[2][MT], w[2][NT];
         decode(0, w[0]);
-        __syncthreads();
-        if (b >= a.blocks) continue;          // (the last turn of some sets)
-        const bool more = b + WK < a.blocks;
-        if (more) fetch(b + WK, buf ^ 1);
+        lds_only_barrier();
+        if (b >= b1) continue;                // (the last turn of some sets)
+        const bool more = b + WK < b1;
+        if (more) {
+            fetch(b + WK, buf ^ 1);
+            load_weights(next);
+        }
         read(0, 0, op[0]);
         typename T::Acc acc[MT][NT] = {};
         // one part of one step after the other; what the next one needs is read and made beside the products
@@ -421,7 +577,7 @@ __global__ void __launch_bounds__(WM * WN * WK * 64, XT == FSCNN_F32 ? 1 : 2) ti
                 }
 #pragma unroll
                 for (int t = 0; t < NT; ++t) {
-                    const float f = __builtin_bit_cast(float, sz[t][g] & ~15u);
+                    const float f = __builtin_bit_cast(float, now.sz[t][g] & ~15u);
 #pragma unroll
                     for (int j = 0; j < 16; ++j) {
                         float v = (float)acc[u][t][j];
@@ -459,6 +615,22 @@ __global__ void __launch_bounds__(WM * WN * WK * 64, XT == FSCNN_F32 ? 1 : 2) ti
 #pragma unroll
                     for (int i = 0; i < 4; ++i) total[e / 4 / NT][e / 4 % NT][e % 4 * 4 + i] += f[i];
                 }
+    }
+    if (gridDim.y > 1) {
+        if (wk == 0)
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                const int k = n0 + 32 * t + (lane & 31);
+                if (k < a.K)
+#pragma unroll
+                    for (int u = 0; u < MT; ++u)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const int m = m0 + wm * (32 * MT) + u * 32 + 8 * (i >> 2) + 4 * half + (i & 3);
+                            if (m < a.M) a.sums[((long long)blockIdx.y * a.M + m) * (a.tiles * 16LL) + k] = total[u][t][i];
+                        }
+            }
+        return;
     }
     // 32 rows of every wave after the other by way of LDS, so that a lane stores 16 bytes of a row of y
     float *const area = reinterpret_cast<float *>(lds);
@@ -505,25 +677,46 @@ __global__ void __launch_bounds__(WM * WN * WK * 64, XT == FSCNN_F32 ? 1 : 2) ti
     }
 }
 
-template <int XT, int NT, int MT, int W> hipError_t launch_rows(const Q4Args &a, int parts, hipStream_t st)
+template <int XT, int NT, int MT, int W> hipError_t launch_rows(const Q4Args &a, hipStream_t st)
 {
     const long long gx = (a.tiles + NT - 1) / NT, gy = ((long long)a.M + 16 * MT - 1) / (16 * MT);
     if (gx * W * 64 > 0xffffffffLL || gy > 65535) return hipErrorInvalidValue;
-    const dim3 grid((unsigned)gx, (unsigned)gy, parts), block(W * 64);
+    const dim3 grid((unsigned)gx, (unsigned)gy), block(W * 64);
     if (a.steps == 1) hipLaunchKernelGGL((rows_kernel<XT, NT, MT, W, 1>), grid, block, 0, st, a);
     else if (a.steps == 2) hipLaunchKernelGGL((rows_kernel<XT, NT, MT, W, 2>), grid, block, 0, st, a);
     else hipLaunchKernelGGL((rows_kernel<XT, NT, MT, W, 4>), grid, block, 0, st, a);
     return hipGetLastError();
 }
 
-template <int XT, int MT, int NT, int WM, int WN, int WK, bool DMA, bool GS> hipError_t launch_tiles(Q4Args a, hipStream_t st)
+template <int XT, int NT, int W> hipError_t launch_staged(const Q4Args &a, hipStream_t st)
+{
+    constexpr int kBytes = XT == FSCNN_I8 ? 1 : 2, kMost = 144 << 10, kTurn = W * kQ4Block;
+    const int rows = a.M * XOp<XT>::kParts;
+    const long long grid = (a.tiles + NT - 1) / NT;
+    if (rows > 16 || grid * W * 64 > 0xffffffffLL) return hipErrorInvalidValue;
+    // as many columns in LDS as leave room for a second work-group where there is one for a CU
+    const int room = grid > 256 ? kMost / 2 : kMost, fit = (room / rows - 16) / kBytes / kTurn * kTurn, all = a.blocks * kQ4Block;
+    const int cols = all < fit ? all : fit, bytes = rows * (cols * kBytes + 16), sums = W * NT * 1024;
+    static_assert(16 * (kTurn * kBytes + 16) <= kMost / 2, "a turn of 16 rows fits");
+    auto launch = [&](auto kernel) {
+        static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, kMost);
+        if (attr != hipSuccess) return attr;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(W * 64), bytes > sums ? bytes : sums, st, a, cols);
+        return hipGetLastError();
+    };
+    if (a.steps == 1) return launch(&staged_kernel<XT, NT, W, 1>);
+    if (a.steps == 2) return launch(&staged_kernel<XT, NT, W, 2>);
+    return launch(&staged_kernel<XT, NT, W, 4>);
+}
+
+template <int XT, int MT, int NT, int WM, int WN, int WK, bool DMA, bool GS> hipError_t launch_tiles(Q4Args a, int parts, hipStream_t st)
 {
     constexpr int rows = 32 * MT * WM, threads = WM * WN * WK * 64;
     const long long mt = ((long long)a.M + rows - 1) / rows, nt = (a.K + 32LL * NT * WN - 1) / (32 * NT * WN);
     if (mt * nt * threads > 0xffffffffLL || 8 * nt > 0x7fffffffLL) return hipErrorInvalidValue;
     a.mt = (int)mt;
     a.nt = (int)nt;
-    const dim3 grid((unsigned)(mt * nt)), block(threads);
+    const dim3 grid((unsigned)(mt * nt), parts), block(threads);
     if (a.steps == 1) hipLaunchKernelGGL((tile_kernel<XT, MT, NT, WM, WN, WK, 1, DMA, GS>), grid, block, 0, st, a);
     else if (a.steps == 2) hipLaunchKernelGGL((tile_kernel<XT, MT, NT, WM, WN, WK, 2, DMA, GS>), grid, block, 0, st, a);
     else hipLaunchKernelGGL((tile_kernel<XT, MT, NT, WM, WN, WK, 4, DMA, GS>), grid, block, 0, st, a);
@@ -533,22 +726,67 @@ template <int XT, int MT, int NT, int WM, int WN, int WK, bool DMA, bool GS> hip
 // x may go to LDS without registers: 16-byte loads, offsets of a tile's rows below 2^31
 inline bool dma_serves(const Q4Args &a, int rows) { return !(((uintptr_t)a.x | (uintptr_t)a.ldx) & 15) && a.ldx * rows < 0x7fff0000LL; }
 
+// Time of a launch in us: 4 and, for every turn (a block a set of waves), `one` while a CU has a work-group, `many` times the work-groups of a CU beyond
+struct TileCost {
+    int rows, cols, sets;
+    float one, many;
+    float us(const Q4Args &a) const
+    {
+        const double groups = (double)((a.M + rows - 1) / rows) * ((a.K + cols - 1) / cols), n = __builtin_ceil(groups / 256);
+        return 4 + (a.blocks + sets - 1) / sets * (n > 1 && many * (float)n > one ? many * (float)n : one);
+    }
+};
+
 template <int XT, int MT, int NT, int WM, int WN, int WK> hipError_t launch_tiles(const Q4Args &a, hipStream_t st)
 {
     constexpr int rows = 32 * MT * WM;
-    if constexpr (XT == FSCNN_F32) return launch_tiles<XT, MT, NT, WM, WN, WK, false, false>(a, st);
-    else if constexpr (XT == FSCNN_I8) {
+    const bool dma = dma_serves(a, rows);
+    if constexpr (XT == FSCNN_I8) {
         if (a.x_cols > 1)
-            return dma_serves(a, rows) ? launch_tiles<XT, MT, NT, WM, WN, WK, true, true>(a, st) : launch_tiles<XT, MT, NT, WM, WN, WK, false, true>(a, st);
-        return dma_serves(a, rows) ? launch_tiles<XT, MT, NT, WM, WN, WK, true, false>(a, st) : launch_tiles<XT, MT, NT, WM, WN, WK, false, false>(a, st);
-    } else {
-        return dma_serves(a, rows) ? launch_tiles<XT, MT, NT, WM, WN, WK, true, false>(a, st) : launch_tiles<XT, MT, NT, WM, WN, WK, false, false>(a, st);
+            return dma ? launch_tiles<XT, MT, NT, WM, WN, WK, true, true>(a, 1, st) : launch_tiles<XT, 2, 1, 1, 4, 1, false, true>(a, 1, st);
+    }
+    return dma ? launch_tiles<XT, MT, NT, WM, WN, WK, true, false>(a, 1, st) : launch_tiles<XT, 2, 1, 1, 4, 1, false, false>(a, 1, st);
+}
+
+// x in 16 or 8 bits.  The fastest of five shapes of tile_kernel by what launches of them take (fitted to 1 to 4096 rows, 1024 to 16384 columns, 1024 to
+// 12288 weight rows, within 15 %): many sets where few work-groups are there, whose sums through LDS cost more than they bring
+// where they are many (bf16, 4096 -> 4096: 64 rows of x 9.3 us with 32 x 32 in 8 sets, 28 with 64 x 128 in one; 1024 rows 117 and 45).  Rows of x that
+// are not 16 bytes aligned come by way of registers and have one shape.  Up to 16 rows also staged_kernel and, for one or two rows, whose operand is
+// not worth a barrier, rows_kernel (bf16, 4096 -> 4096: one row 3.7 us, 4.1 staged; 8 rows 5.5 and 4.9).  Sixteen waves where a wave of
+// eight had eight blocks or more (one row of 16384: 8.3 us, 10.3 with eight; of 4096: 3.9 and 3.7).
+template <int XT> hipError_t launch_narrow(const Q4Args &a, hipStream_t st)
+{
+    constexpr bool kInt = XT == FSCNN_I8;
+    constexpr TileCost kTiles[5] = {{32, 32, 8, kInt ? 0.68f : 1.3f, kInt ? 0.8f : 1.55f}, {32, 64, 4, kInt ? 0.6f : 1.0f, kInt ? 0.6f : 0.93f},
+                                    {64, 128, 2, kInt ? 0.8f : 1.3f, kInt ? 0.79f : 1.42f}, {64, 128, 1, kInt ? 0.52f : 0.8f, kInt ? 0.41f : 0.62f},
+                                    {128, 128, 1, kInt ? 0.9f : 1.25f, kInt ? 0.72f : 1.08f}};
+    int best = 0;
+    float us = kTiles[0].us(a);
+    for (int i = 1; i < 5; ++i)
+        if (const float t = kTiles[i].us(a); t < us) {
+            us = t;
+            best = i;
+        }
+    if (a.M <= 16) {
+        const int n = (a.tiles + 255) / 256;
+        const bool deep = a.blocks >= 64 && n == 1;
+        if (a.M <= 4 || 2.9f + n * (a.blocks / 32.0f) * (0.95f + 0.13f * a.M) <= us) {
+            if (a.M > 2) return deep ? launch_staged<XT, 1, 16>(a, st) : launch_staged<XT, 1, 8>(a, st);
+            return deep ? launch_rows<XT, 1, 1, 16>(a, st) : launch_rows<XT, 1, 1, 8>(a, st);
+        }
+    }
+    switch (best) {
+        case 0: return launch_tiles<XT, 1, 1, 1, 1, 8>(a, st);
+        case 1: return launch_tiles<XT, 1, 1, 1, 2, 4>(a, st);
+        case 2: return launch_tiles<XT, 2, 1, 1, 4, 2>(a, st);
+        case 3: return launch_tiles<XT, 2, 1, 1, 4, 1>(a, st);
+        default: return launch_tiles<XT, 4, 1, 1, 4, 1>(a, st);
     }
 }
 
 }  // namespace
 
-// parts: as q4_parts() says, or 1
+// parts: work-groups that divide the columns (32-bit floats: q4_parts(); else 1)
 template <int XT> hipError_t launch_q4_type(const Q4Args &a, int parts, hipStream_t st);
 template <> hipError_t launch_q4_type<FSCNN_F32>(const Q4Args &a, int parts, hipStream_t st);
 template <> hipError_t launch_q4_type<FSCNN_F16>(const Q4Args &a, int parts, hipStream_t st);

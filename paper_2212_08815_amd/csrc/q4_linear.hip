@@ -5,6 +5,8 @@ namespace fscnn {
 
 namespace {
 
+constexpr int kQ4LaunchRows = 1 << 18;
+
 // What the work-groups that divide the columns have left, added in their order; a thread an output
 __global__ void __launch_bounds__(256) join_kernel(const Q4Args a, int parts)
 {
@@ -23,23 +25,18 @@ __global__ void __launch_bounds__(256) join_kernel(const Q4Args a, int parts)
 
 int q4_parts(const fscnn_q4 *q, int x_type, int M)
 {
-    // Floats are taken apart by every wave that reads them, which 64 rows of weights a wave pay for: then a few rows of x leave too few work-groups,
-    // and up to eight divide the columns, four blocks a wave or more.
-    if (x_type != FSCNN_F32 || M > 64) return 1;
-    const long long tiles = q4_tiles(q->K), groups = (tiles + 3) / 4;
-    const int blocks = (int)q4_blocks(q->C);
-    if (M <= 16 && tiles * blocks < 8192) return 1;
-    int parts = 1;
-    while (parts < 8 && groups * parts < 256 && blocks / (2 * parts) >= 8) parts *= 2;
-    return parts;
+    // (a launch's rows of x: the sums' room is for one launch, and bounded)
+    constexpr double kMostBytes = 64 << 20;
+    if (x_type != FSCNN_F32 || M <= 0 || M > kQ4LaunchRows) return 1;
+    const int most = (int)(kMostBytes / (64.0 * q4_tiles(q->K) * M));
+    return f32_choice(q4_tiles(q->K), (int)q4_blocks(q->C), M, most > 1 ? most : 1).parts;
 }
 
 hipError_t launch_linear_q4(const fscnn_q4 *q, const void *x, int x_type, long long ldx, const float *x_scale, int x_scale_cols, int M,
                             const float *bias, int act, void *y, int y_type, long long ldy, float *sums, hipStream_t st)
 {
     const int bytes = x_type == FSCNN_F32 ? 4 : x_type == FSCNN_I8 ? 1 : 2;
-    // (rows of x in launches that a grid holds)
-    constexpr long long kMost = 1 << 18;
+    constexpr long long kMost = kQ4LaunchRows;   // rows of x in launches that a grid holds
     for (long long m = 0; m < M; m += kMost) {
         const Q4Args a = {reinterpret_cast<const u4v *>(q->codes), q->scales, static_cast<const char *>(x) + m * ldx * bytes,
                           x_scale ? x_scale + m * x_scale_cols : nullptr, bias, static_cast<char *>(y) + m * ldy * (y_type == FSCNN_F32 ? 4 : 2), sums,
