@@ -1,14 +1,19 @@
 // The kernels of y = act(x W^T + b) with 4-bit weights (internal.h has their order, q4_tile.h the operands), for one type of x a translation unit.
 //
-// rows_kernel (few rows of x): a work-group of W waves owns up to 16 MT rows of x and 16 NT rows of weights.  Both go straight from memory into the
-// matrix cores' operands (16 bytes a lane hold the codes of 16 rows x 128 columns), the next block's loads on their way while one is computed.
-// The waves divide the blocks of 128 columns, each keeps fp32 sums of its own, which are added at the end through LDS in the order of the
-// waves.  Several work-groups may divide the blocks once more; then they leave their sums for join_kernel (q4_linear.hip).
+// rows_kernel (one or two rows of x; fp32 also six to 16 of little work) and staged_kernel (up to 16 rows, in fp32 five): a work-group of W waves owns
+// 16 rows of weights, whose codes go straight from memory into the matrix cores' operands (16 bytes a lane hold 16 rows x 128 columns), as do
+// the rows of x or, in staged_kernel, from LDS.  The waves divide the blocks of 128 columns, each keeps fp32 sums of its own, which are
+// added at the end through LDS.  What bounds them: a launch and two trips to memory where the weights are few (4096 x 4096, one row of bf16: 3.7 us,
+// 2.3 TB/s), else vector instructions and the codes' way (25088 x 4096, one row of fp32: 13.3 us, 4.0 TB/s).
 //
-// tile_kernel (many rows of x): WM x WN waves own 32 MT WM rows of x and 32 NT WN rows of weights.  A block of 128 columns of the rows
-// of x is in LDS while the next one is on its way there (16 bytes a lane, without registers where x is aligned); codes come from memory into
-// registers a block ahead.  What a wave does per block: 8 MT NT products of 32 x 32 x 16, codes to operands, and a multiply-add per output and
-// group, since a group's sum is multiplied by its scale in fp32.  WK such sets of waves may divide the blocks; their sums are added through LDS.
+// tile_kernel (many rows of x): WN waves, a set, own 32 MT rows of x and 32 WN rows of weights.  A block of 128 columns of the rows of x is in LDS
+// while the next one is on its way there (16 bytes a lane, without registers where x is aligned); codes come from memory into registers a
+// block ahead.  WK sets may divide the blocks; their sums are added through LDS.  What a wave does per block (16 bits, MT = 4): 32 products of
+// 32 x 32 x 16, 1024 clocks of the matrix core, 19 vector instructions for every 8 codes a lane, 152, and 64 multiply-adds, since a
+// group's sum is multiplied by its scale in fp32; with addresses and staging 263.  The two hardly overlap, on one wave or on two
+// (counted: 4350 clocks of a SIMD per two such blocks, 2048 of products and 2100 of vector instructions), so what counts is how few of
+// the latter there are: hence 128 rows of x per decoded weight.  4096 rows of 4096 x 12288, bf16: 415 us, 0.99 PFLOP/s; without the
+// stores 375, without decoding 330.  Decoding for twice the rows at once, or a second block of codes ahead, brought nothing.
 #pragma once
 #include <type_traits>
 
@@ -63,104 +68,98 @@ __device__ inline void store_output(const Q4Args &a, int m, int k, float v, floa
     store_float(a.y, m * a.ldy + k, a.y_type, act_apply(v + bias, a.act));
 }
 
-template <int XT, int NT, int MT, int W, int STEPS> __global__ void __launch_bounds__(W * 64) rows_kernel(const Q4Args a)
+// The scales of a group of rows m to m + 3 of x, where x has one for each group
+template <int XT> __device__ inline q4f4 row_scales(const Q4Args &a, int m, int group)
+{
+    q4f4 xs = {1.0f, 1.0f, 1.0f, 1.0f};
+    if (XT == FSCNN_I8 && a.x_cols > 1) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) xs[i] = m + i < a.M && group < a.x_cols ? a.x_scale[(long long)(m + i) * a.x_cols + group] : 0.0f;
+    }
+    return xs;
+}
+
+// A group's end in the 16-row kernels: its sum without the zero point's share, times its scale (and, in 8 bits, those of x).  acc, sum: products with
+// the codes and with ones
+template <int XT, class Acc> __device__ inline q4f4 add_group(const q4f4 &xs, uint32_t word, const Acc &acc, const Acc &sum, q4f4 total)
+{
+    const float f = __builtin_bit_cast(float, word & ~15u), z = -(float)(word & 15);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float v;
+        if constexpr (XT == FSCNN_I8) {
+            v = (float)(acc[i] - (int)(word & 15) * sum[i]) * xs[i];
+        } else {
+            v = __builtin_fmaf(z, sum[i], acc[i]);
+        }
+        total[i] = __builtin_fmaf(f, v, total[i]);
+    }
+    return total;
+}
+
+// The outputs of 16 rows of weights from the sums of W waves, [W][64 lanes][4 rows of the operand], PARTS rows of which are one of x: added in the
+// order of parts and waves
+template <int XT, int PARTS, int W> __device__ inline void store_sums(const Q4Args &a, const float *sums, int tile)
+{
+    for (int e = threadIdx.x; e < a.M * 16; e += W * 64) {
+        const int m = e >> 4, k = tile * 16 + (e & 15);
+        float f = 0.0f;
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p) {
+            const int row = m * PARTS + p, at = ((row >> 2) * 16 + (e & 15)) * 4 + (row & 3);
+#pragma unroll
+            for (int w = 0; w < W; ++w) f += sums[w * 256 + at];
+        }
+        if (k >= a.K) continue;
+        store_output(a, m, k, XT == FSCNN_I8 && a.x_cols == 1 ? f * a.x_scale[m] : f, a.bias ? a.bias[k] : 0.0f);
+    }
+}
+
+// 16 rows of weights, W waves
+template <int XT, int W, int STEPS> __global__ void __launch_bounds__(W * 64) rows_kernel(const Q4Args a)
 {
     using X = XOp<XT>;
-    constexpr bool kInt = XT == FSCNN_I8;
     constexpr int kGroups = 4 / STEPS;        // of a block
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int col16 = lane & 15, quarter = lane >> 4;
-    const int tile0 = blockIdx.x * NT, m0 = blockIdx.y * (16 * MT);
-    const u4v *codes[NT];
-    const uint32_t *scales[NT];
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {            // (tiles past the last one repeat it, and so do rows of x: their outputs are not stored)
-        const long long tile = tile0 + t < a.tiles ? tile0 + t : a.tiles - 1;
-        codes[t] = a.codes + tile * a.blocks * 64 + lane;
-        scales[t] = a.scales + tile * a.blocks * (kGroups * 16) + col16;
-    }
-    const char *rows[MT];
-#pragma unroll
-    for (int u = 0; u < MT; ++u) {
-        const int m = m0 + 16 * u + col16;
-        rows[u] = a.x + (m < a.M ? m : a.M - 1) * a.ldx;
-    }
-    q4f4 total[NT][MT] = {};
+    const int col16 = lane & 15, quarter = lane >> 4, tile = blockIdx.x;
+    const u4v *codes = a.codes + (long long)tile * a.blocks * 64 + lane;
+    const uint32_t *scales = a.scales + (long long)tile * a.blocks * (kGroups * 16) + col16;
+    const char *row = a.x + (col16 < a.M ? col16 : a.M - 1) * a.ldx;   // (rows past the last one repeat it: their outputs are not stored)
     struct Weights {
-        u4v w[NT];
-        uint32_t sz[NT][kGroups];
+        u4v w;
+        uint32_t sz[kGroups];
     };
     auto load_weights = [&](int b, Weights &v) {
+        v.w = codes[(long long)b * 64];
 #pragma unroll
-        for (int t = 0; t < NT; ++t) v.w[t] = codes[t][(long long)b * 64];
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-            for (int g = 0; g < kGroups; ++g) v.sz[t][g] = scales[t][((long long)b * kGroups + g) * 16];
+        for (int g = 0; g < kGroups; ++g) v.sz[g] = scales[((long long)b * kGroups + g) * 16];
     };
-    typename X::Raw raw[4][MT];
-    auto load_x = [&](int b, int s, auto tail) {
-#pragma unroll
-        for (int u = 0; u < MT; ++u) raw[s][u] = load_columns<XT, decltype(tail)::value>(rows[u], b * kQ4Block + s * 32 + quarter * 8, a.C);
-    };
+    typename X::Raw raw[4];
+    auto load_x = [&](int b, int s, auto tail) { raw[s] = load_columns<XT, decltype(tail)::value>(row, b * kQ4Block + s * 32 + quarter * 8, a.C); };
+    q4f4 total = {};
     // block b; its loads are done or on their way, those of block `then` are issued here if there is one
     auto block = [&](int b, int then, const Weights &v, Weights &next, auto has) {
         if constexpr (decltype(has)::value) load_weights(then, next);
-        typename X::Acc acc[NT][MT] = {}, sum[MT] = {};
+        q4f4 xs[kGroups];
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) xs[g] = row_scales<XT>(a, 4 * quarter, b * kGroups + g);
+        typename X::Acc acc = {}, sum = {};
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
-            typename X::Op op[MT][X::kParts];
-#pragma unroll
-            for (int u = 0; u < MT; ++u) X::parts(raw[s][u], op[u]);
+            typename X::Op op[X::kParts];
+            X::parts(raw[s], op);
             if constexpr (decltype(has)::value) load_x(then, s, std::false_type{});
-            typename X::Op q[NT];
+            const typename X::Op q = X::codes(v.w[s]);
 #pragma unroll
-            for (int t = 0; t < NT; ++t) q[t] = X::codes(v.w[t][s]);
-            // (parts outermost: products that follow each other add to different sums)
-#pragma unroll
-            for (int p = 0; p < X::kParts; ++p)
-#pragma unroll
-                for (int u = 0; u < MT; ++u) {
-                    sum[u] = X::mfma(op[u][p], X::ones(), sum[u]);
-#pragma unroll
-                    for (int t = 0; t < NT; ++t) acc[t][u] = X::mfma(op[u][p], q[t], acc[t][u]);
-                }
+            for (int p = 0; p < X::kParts; ++p) {
+                sum = X::mfma(op[p], X::ones(), sum);
+                acc = X::mfma(op[p], q, acc);
+            }
             if ((s + 1) % STEPS == 0) {       // the group's end
-                const int g = b * kGroups + s / STEPS;
-                q4f4 xs[MT];
-#pragma unroll
-                for (int u = 0; u < MT; ++u)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        xs[u][i] = 1.0f;
-                        if (kInt && a.x_cols > 1) {
-                            const int m = m0 + 16 * u + 4 * quarter + i;
-                            if (m < a.M && g < a.x_cols) xs[u][i] = a.x_scale[(long long)m * a.x_cols + g];
-                        }
-                    }
-#pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    const uint32_t sz = v.sz[t][s / STEPS];
-                    const float f = __builtin_bit_cast(float, sz & ~15u), z = -(float)(sz & 15);
-#pragma unroll
-                    for (int u = 0; u < MT; ++u) {
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            float w;
-                            if constexpr (kInt) w = (float)(acc[t][u][i] - (int)(sz & 15) * sum[u][i]) * xs[u][i];
-                            else w = __builtin_fmaf(z, sum[u][i], acc[t][u][i]);
-                            total[t][u][i] = __builtin_fmaf(f, w, total[t][u][i]);
-                        }
-                        acc[t][u] = {};
-                    }
-                }
-#pragma unroll
-                for (int u = 0; u < MT; ++u) sum[u] = {};
-                // (a second group's sums at the same time would not fit the registers)
-#pragma unroll
-                for (int t = 0; t < NT; ++t)
-#pragma unroll
-                    for (int u = 0; u < MT; ++u) asm volatile("" : "+v"(total[t][u]));
+                total = add_group<XT>(xs[s / STEPS], v.sz[s / STEPS], acc, sum, total);
+                acc = sum = typename X::Acc{};
+                // (a second group's sums at the same time would take more registers)
+                asm volatile("" : "+v"(total));
             }
         }
     };
@@ -184,70 +183,45 @@ template <int XT, int NT, int MT, int W, int STEPS> __global__ void __launch_bou
         for (int s = 0; s < 4; ++s) load_x(b, s, std::true_type{});
         block(b, 0, v, next, std::false_type{});
     }
-
-    __shared__ q4f4 sums[W][NT * MT][64];
-#pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int u = 0; u < MT; ++u) sums[wave][t * MT + u][lane] = total[t][u];
+    __shared__ q4f4 sums[W][64];
+    sums[wave][lane] = total;
     __syncthreads();
-    for (int e = wave; e < NT * MT; e += W) {
-        q4f4 f = sums[0][e][lane];
-#pragma unroll
-        for (int i = 1; i < W; ++i) f += sums[i][e][lane];
-        const int m = m0 + e % MT * 16 + 4 * quarter, k = (tile0 + e / MT) * 16 + col16;
-        if (k >= a.K) continue;
-        const float bias = a.bias ? a.bias[k] : 0.0f;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (m + i < a.M) store_output(a, m + i, k, kInt && a.x_cols == 1 ? f[i] * a.x_scale[m + i] : f[i], bias);
-    }
+    store_sums<XT, 1, W>(a, reinterpret_cast<const float *>(sums), tile);
 }
 
 // Few rows of x: all of them, each of their parts, are the 16 rows of one operand, so that a row of x costs a third of a product and not three.  The
 // operand is made once for a work-group: `cols` columns at a time lie in LDS, rows 16 bytes more than that apart (a multiple of 256 bytes:
-// the 16 rows of a chunk are in all banks).  NT tiles of weights, W waves that divide the blocks; their sums are added as rows_kernel adds them.
+// the 16 rows of a chunk are in all banks).  16 rows of weights, W waves that divide the blocks; their sums are added as rows_kernel adds them.
 template <int XT> using RowOp = XOp<XT == FSCNN_F32 ? FSCNN_BF16 : XT>;
-template <int XT, int NT, int W, int STEPS> __global__ void __launch_bounds__(W * 64) staged_kernel(const Q4Args a, int cols)
+template <int XT, int W, int STEPS> __global__ void __launch_bounds__(W * 64) staged_kernel(const Q4Args a, int cols)
 {
     using X = XOp<XT>;
     using R = RowOp<XT>;
-    constexpr bool kInt = XT == FSCNN_I8;
-    constexpr int kGroups = 4 / STEPS, kBytes = kInt ? 1 : 2, kParts = X::kParts;
+    constexpr int kGroups = 4 / STEPS, kBytes = XT == FSCNN_I8 ? 1 : 2, kParts = X::kParts;
     extern __shared__ __align__(256) char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int col16 = lane & 15, quarter = lane >> 4;
-    const int tile0 = blockIdx.x * NT, pitch = cols * kBytes + 16;
-    const u4v *codes[NT];
-    const uint32_t *scales[NT];
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {            // (tiles past the last one repeat it: their outputs are not stored)
-        const long long tile = tile0 + t < a.tiles ? tile0 + t : a.tiles - 1;
-        codes[t] = a.codes + tile * a.blocks * 64 + lane;
-        scales[t] = a.scales + tile * a.blocks * (kGroups * 16) + col16;
-    }
+    const int col16 = lane & 15, quarter = lane >> 4, tile = blockIdx.x, pitch = cols * kBytes + 16;
+    const u4v *codes = a.codes + (long long)tile * a.blocks * 64 + lane;
+    const uint32_t *scales = a.scales + (long long)tile * a.blocks * (kGroups * 16) + col16;
     struct Weights {
-        u4v w[NT];
-        uint32_t sz[NT][kGroups];
+        u4v w;
+        uint32_t sz[kGroups];
     };
     auto load_weights = [&](int b, Weights &v) {
+        b = b < a.blocks ? b : a.blocks - 1;
+        v.w = codes[(long long)b * 64];
 #pragma unroll
-        for (int t = 0; t < NT; ++t) v.w[t] = codes[t][(long long)b * 64];
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-            for (int g = 0; g < kGroups; ++g) v.sz[t][g] = scales[t][((long long)b * kGroups + g) * 16];
+        for (int g = 0; g < kGroups; ++g) v.sz[g] = scales[((long long)b * kGroups + g) * 16];
     };
     const int rows = a.M * kParts;            // at most 16; the operand's others repeat the last one
     const char *mine = lds + (col16 < rows ? col16 : rows - 1) * pitch + quarter * (8 * kBytes);
-    q4f4 total[NT] = {};
+    q4f4 total = {};
     // Codes are two blocks ahead, in three slots.  (Every step loads, past the last block that one again: the waits count loads.)
     Weights v[3];
-    auto block_at = [&](int i) { return i < a.blocks ? i : a.blocks - 1; };
     int b = wave;
     for (int c0 = 0; c0 < a.blocks * kQ4Block; c0 += cols) {
-        load_weights(block_at(b), v[0]);
-        load_weights(block_at(b + W), v[1]);
+        load_weights(b, v[0]);
+        load_weights(b + W, v[1]);
         if (c0) __syncthreads();
         const int end = a.blocks * kQ4Block - c0 < cols ? a.blocks * kQ4Block - c0 : cols;
         const int inside = a.C - c0 < end ? (a.C - c0) & ~7 : end;   // columns in whole chunks of 8; then those that end in C, and zeros
@@ -278,43 +252,22 @@ template <int XT, int NT, int W, int STEPS> __global__ void __launch_bounds__(W 
         }
         __syncthreads();
         auto block = [&](const Weights &now, Weights &after) {
-            load_weights(block_at(b + 2 * W), after);
-            q4f4 xs[kInt ? kGroups : 1];
-            if constexpr (kInt) {
+            load_weights(b + 2 * W, after);
+            q4f4 xs[kGroups];
 #pragma unroll
-                for (int g = 0; g < kGroups; ++g)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        xs[g][i] = 1.0f;
-                        const int m = 4 * quarter + i, group = b * kGroups + g;
-                        if (a.x_cols > 1 && m < a.M && group < a.x_cols) xs[g][i] = a.x_scale[(long long)m * a.x_cols + group];
-                    }
-            }
+            for (int g = 0; g < kGroups; ++g) xs[g] = row_scales<XT>(a, 4 * quarter, b * kGroups + g);
             const char *from = mine + (b * kQ4Block - c0) * kBytes;
             typename R::Op op[4];
 #pragma unroll
             for (int s = 0; s < 4; ++s) op[s] = *reinterpret_cast<const typename R::Op *>(from + s * (32 * kBytes));
-            typename R::Acc acc[NT] = {}, sum = {};
+            typename R::Acc acc = {}, sum = {};
 #pragma unroll
             for (int s = 0; s < 4; ++s) {
                 sum = R::mfma(op[s], R::ones(), sum);
-#pragma unroll
-                for (int t = 0; t < NT; ++t) acc[t] = R::mfma(op[s], R::codes(now.w[t][s]), acc[t]);
+                acc = R::mfma(op[s], R::codes(now.w[s]), acc);
                 if ((s + 1) % STEPS == 0) {
-#pragma unroll
-                    for (int t = 0; t < NT; ++t) {
-                        const uint32_t sz = now.sz[t][s / STEPS];
-                        const float f = __builtin_bit_cast(float, sz & ~15u), z = -(float)(sz & 15);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            float w;
-                            if constexpr (kInt) w = (float)(acc[t][i] - (int)(sz & 15) * sum[i]) * xs[s / STEPS][i];
-                            else w = __builtin_fmaf(z, sum[i], acc[t][i]);
-                            total[t][i] = __builtin_fmaf(f, w, total[t][i]);
-                        }
-                        acc[t] = typename R::Acc{};
-                    }
-                    sum = typename R::Acc{};
+                    total = add_group<XT>(xs[s / STEPS], now.sz[s / STEPS], acc, sum, total);
+                    acc = sum = typename R::Acc{};
                 }
             }
             b += W;
@@ -324,22 +277,10 @@ template <int XT, int NT, int W, int STEPS> __global__ void __launch_bounds__(W 
             while (block(v[0], v[2]) && block(v[1], v[0]) && block(v[2], v[1])) {}
     }
     __syncthreads();
-    float *const sums = reinterpret_cast<float *>(lds);   // [W][NT][64 lanes][4]
-#pragma unroll
-    for (int t = 0; t < NT; ++t) *reinterpret_cast<q4f4 *>(sums + ((wave * NT + t) * 64 + lane) * 4) = total[t];
+    q4f4 *const sums = reinterpret_cast<q4f4 *>(lds);   // [W][64 lanes]
+    sums[wave * 64 + lane] = total;
     __syncthreads();
-    for (int e = threadIdx.x; e < a.M * (16 * NT); e += W * 64) {
-        const int m = e / (16 * NT), t = e / 16 % NT, k = (tile0 + t) * 16 + (e & 15);
-        float f = 0.0f;
-#pragma unroll
-        for (int p = 0; p < kParts; ++p) {
-            const int row = m * kParts + p, at = ((row >> 2) * 16 + (e & 15)) * 4 + (row & 3);
-#pragma unroll
-            for (int w = 0; w < W; ++w) f += sums[(w * NT + t) * 256 + at];
-        }
-        if (k >= a.K) continue;
-        store_output(a, m, k, kInt && a.x_cols == 1 ? f * a.x_scale[m] : f, a.bias ? a.bias[k] : 0.0f);
-    }
+    store_sums<XT, kParts, W>(a, reinterpret_cast<const float *>(sums), tile);
 }
 
 // The 32 x 32 products: 16 columns in 16 bits, 32 in 8
@@ -371,31 +312,31 @@ __device__ inline int xcd_neighbours(int bid, int nblk)
 // STEPS: of 32 columns a group.  DMA: rows of x are 16 bytes aligned, offsets in a tile below 2^31.  GS: x (8 bits) has a scale for each group.
 // x in LDS: rows of kChunks 16-byte chunks a part, chunk c of row r at c ^ f(r), so that the 16 lanes that read a chunk of adjacent rows find
 // it in all banks.
-template <int XT, int MT, int NT, int WM, int WN, int WK, int STEPS, bool DMA, bool GS>
-__global__ void __launch_bounds__(WM * WN * WK * 64, XT == FSCNN_F32 ? 1 : 2) tile_kernel(const Q4Args a)
+template <int XT, int MT, int WN, int WK, int STEPS, bool DMA, bool GS>
+__global__ void __launch_bounds__(WN * WK * 64, XT == FSCNN_F32 ? 1 : 2) tile_kernel(const Q4Args a)
 {
     using X = XOp<XT>;
     using T = Tile<XT>;
     constexpr bool kInt = XT == FSCNN_I8;
-    constexpr int kRows = 32 * MT * WM, kSet = WM * WN * 64, kParts = X::kParts, kCh = T::kChunks, kGroups = 4 / STEPS;
+    constexpr int kRows = 32 * MT, kSet = WN * 64, kParts = X::kParts, kCh = T::kChunks, kGroups = 4 / STEPS;
     constexpr int kAnyAlu = 6;                            // of sched_barrier: vector and scalar arithmetic may pass
     constexpr int kSteps = kInt ? 4 : 8, kStepsOfGroup = kSteps / kGroups;   // products of a block, of a group
     constexpr int kPer = kRows * kCh / kSet;              // chunks a thread brings
     constexpr int kBuf = kRows * kCh * kParts;            // chunks of a buffer
     constexpr int kScales = GS ? 2 * kGroups * kRows / 4 : 0;
-    constexpr int kSums = (WK - 1) * kSet * MT * NT * 4;  // in 16 bytes, at the end
+    constexpr int kSums = (WK - 1) * kSet * MT * 4;  // in 16 bytes, at the end
     constexpr int kChunksOfSet = 2 * kBuf + kScales;
     static_assert(kPer * kSet == kRows * kCh, "a whole number of chunks a thread");
     static_assert(!GS || kRows <= kSet, "a thread a row");
-    constexpr int kPitch = 32 * NT * WN + 8, kArea = 32 * WM * kPitch;   // of outputs, in floats: rows 4 apart half of the banks apart
+    constexpr int kPitch = 32 * WN + 8, kArea = 32 * kPitch;   // of outputs, in floats: rows 4 apart half of the banks apart
     constexpr int kNeed = kSums * 4 > 2 * kArea ? kSums : (2 * kArea + 3) / 4;
     __shared__ u4v lds[kChunksOfSet * WK > kNeed ? kChunksOfSet * WK : kNeed];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int wk = wave / (WM * WN), in_set = wave % (WM * WN), half = lane >> 5, wm = in_set / WN, wn = in_set % WN;
+    const int wk = wave / WN, in_set = wave % WN, half = lane >> 5;
     // panels of 8 tiles of x: work-groups that run together share both operands
     const int lid = xcd_neighbours(blockIdx.x, a.mt * a.nt), panel = lid / (8 * a.nt), in = lid % (8 * a.nt);
     const int tall = a.mt - panel * 8 < 8 ? a.mt - panel * 8 : 8;
-    const int m0 = (panel * 8 + in % tall) * kRows, n0 = in / tall * (32 * NT * WN) + wn * (32 * NT);
+    const int m0 = (panel * 8 + in % tall) * kRows, n0 = in / tall * (32 * WN) + in_set * 32;
     auto swizzle = [](int r) { return kCh == 16 ? r & 15 : r >> 1 & 7; };
 
     // codes and scales: a base for the wave, which moves from block to block, and what a lane is away from it
@@ -404,14 +345,9 @@ __global__ void __launch_bounds__(WM * WN * WK * 64, XT == FSCNN_F32 ? 1 : 2) ti
     const int b0 = (int)((long long)a.blocks * blockIdx.y / gridDim.y), b1 = (int)((long long)a.blocks * (blockIdx.y + 1) / gridDim.y);
     const char *codes = reinterpret_cast<const char *>(a.codes) + ((long long)first * a.blocks + b0 + wk) * 1024;
     const char *scales = reinterpret_cast<const char *>(a.scales) + ((long long)first * a.blocks + b0 + wk) * (kGroups * 64);
-    uint32_t code_at[NT], scale_at[NT];
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {            // (tiles past the last one repeat it: their outputs are not stored)
-        int tile = (n0 + 32 * t + (lane & 31)) >> 4;
-        tile = (tile < a.tiles ? tile : a.tiles - 1) - first;
-        code_at[t] = tile * a.blocks * 1024 + ((lane & 15) + 32 * half) * 16;
-        scale_at[t] = tile * a.blocks * (kGroups * 64) + (lane & 15) * 4;
-    }
+    // (tiles past the last one repeat it: their outputs are not stored)
+    const int behind = (n0 + (lane & 31)) >> 4 < a.tiles ? ((n0 + (lane & 31)) >> 4) - first : a.tiles - 1 - first;
+    const uint32_t code_at = behind * a.blocks * 1024 + ((lane & 15) + 32 * half) * 16, scale_at = behind * a.blocks * (kGroups * 64) + (lane & 15) * 4;
     const int live = a.M - m0 < kRows ? a.M - m0 : kRows;
     const char *x = a.x + m0 * a.ldx;
     u4v *const set = lds + wk * kChunksOfSet;
@@ -451,17 +387,14 @@ __global__ void __launch_bounds__(WM * WN * WK * 64, XT == FSCNN_F32 ? 1 : 2) ti
     Chunk raw[DMA ? 1 : kPer];
     float xs_next[GS ? kGroups : 1];
     struct Weights {
-        u4v w[NT][2];
-        uint32_t sz[NT][kGroups];
+        u4v w[2];
+        uint32_t sz[kGroups];
     } now, next;
     auto load_weights = [&](Weights &v) {
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
+        for (int e = 0; e < 2; ++e) v.w[e] = *reinterpret_cast<const u4v *>(codes + (code_at + 256 * e));
 #pragma unroll
-            for (int e = 0; e < 2; ++e) v.w[t][e] = *reinterpret_cast<const u4v *>(codes + (code_at[t] + 256 * e));
-#pragma unroll
-            for (int g = 0; g < kGroups; ++g) v.sz[t][g] = *reinterpret_cast<const uint32_t *>(scales + (scale_at[t] + 64 * g));
-        }
+        for (int g = 0; g < kGroups; ++g) v.sz[g] = *reinterpret_cast<const uint32_t *>(scales + (scale_at + 64 * g));
         codes += WK * 1024;
         scales += WK * (kGroups * 64);
     };
@@ -507,8 +440,8 @@ __global__ void __launch_bounds__(WM * WN * WK * 64, XT == FSCNN_F32 ? 1 : 2) ti
                 for (int g = 0; g < kGroups; ++g) set_scales[(buf * kGroups + g) * kRows + r] = xs_next[g];
         }
     };
-    q4f16 total[MT][NT] = {};
-    const int row0 = wm * (32 * MT) + (lane & 31);
+    q4f16 total[MT] = {};
+    const int row0 = lane & 31;
     const int turns = (b1 - b0 + WK - 1) / WK;
 
     if (b0 + wk < b1) {
@@ -521,16 +454,13 @@ __global__ void __launch_bounds__(WM * WN * WK * 64, XT == FSCNN_F32 ? 1 : 2) ti
         wait_vmcnt<0>();                      // the block is in LDS, its codes in registers
         now = next;
         // step st of the block: the weights' operand
-        auto decode = [&](int st, u4v *w) {
-#pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                const typename X::Zero z = X::zero(now.sz[t][st / kStepsOfGroup]);
-                if constexpr (kInt) {
-                    const u2v w0 = X::weights(now.w[t][0][st], z), w1 = X::weights(now.w[t][1][st], z);
-                    w[t] = u4v{w0[0], w0[1], w1[0], w1[1]};
-                } else {
-                    w[t] = X::weights(now.w[t][st & 1][st >> 1], z);
-                }
+        auto decode = [&](int st) {
+            const typename X::Zero z = X::zero(now.sz[st / kStepsOfGroup]);
+            if constexpr (kInt) {
+                const u2v w0 = X::weights(now.w[0][st], z), w1 = X::weights(now.w[1][st], z);
+                return u4v{w0[0], w0[1], w1[0], w1[1]};
+            } else {
+                return X::weights(now.w[st & 1][st >> 1], z);
             }
         };
         const u4v *from_lds = set + buf * kBuf + row0 * kCh;
@@ -540,8 +470,8 @@ __global__ void __launch_bounds__(WM * WN * WK * 64, XT == FSCNN_F32 ? 1 : 2) ti
 #pragma unroll
             for (int u = 0; u < MT; ++u) op[u] = from_lds[p * kRows * kCh + u * 32 * kCh + (chunk ^ swizzle(row0))];
         };
-        u4v op[2][MT], w[2][NT];
-        decode(0, w[0]);
+        u4v op[2][MT], w[2];
+        w[0] = decode(0);
         lds_only_barrier();
         if (b >= b1) continue;                // (the last turn of some sets)
         const bool more = b + WK < b1;
@@ -550,7 +480,7 @@ __global__ void __launch_bounds__(WM * WN * WK * 64, XT == FSCNN_F32 ? 1 : 2) ti
             load_weights(next);
         }
         read(0, 0, op[0]);
-        typename T::Acc acc[MT][NT] = {};
+        typename T::Acc acc[MT] = {};
         // one part of one step after the other; what the next one needs is read and made beside the products
 #pragma unroll
         for (int i = 0; i < kSteps * kParts; ++i) {
@@ -559,10 +489,8 @@ __global__ void __launch_bounds__(WM * WN * WK * 64, XT == FSCNN_F32 ? 1 : 2) ti
             if (!last) read((i + 1) / kParts, (i + 1) % kParts, op[(i + 1) & 1]);
             __builtin_amdgcn_sched_barrier(kAnyAlu);   // (else the reads sink to their uses, to save registers)
 #pragma unroll
-            for (int u = 0; u < MT; ++u)
-#pragma unroll
-                for (int t = 0; t < NT; ++t) acc[u][t] = T::mfma(op[i & 1][u], w[st & 1][t], acc[u][t]);
-            if (!last && p == kParts - 1) decode(st + 1, w[(st + 1) & 1]);
+            for (int u = 0; u < MT; ++u) acc[u] = T::mfma(op[i & 1][u], w[st & 1], acc[u]);
+            if (!last && p == kParts - 1) w[(st + 1) & 1] = decode(st + 1);
             __builtin_amdgcn_sched_barrier(kAnyAlu);
             if (p != kParts - 1 || (st + 1) % kStepsOfGroup) continue;
             // the group's end
@@ -573,25 +501,20 @@ __global__ void __launch_bounds__(WM * WN * WK * 64, XT == FSCNN_F32 ? 1 : 2) ti
                 if constexpr (GS) {
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
-                        xs[j] = *reinterpret_cast<const q4f4 *>(set_scales + (buf * kGroups + g) * kRows + wm * (32 * MT) + u * 32 + 8 * j + 4 * half);
+                        xs[j] = *reinterpret_cast<const q4f4 *>(set_scales + (buf * kGroups + g) * kRows + u * 32 + 8 * j + 4 * half);
                 }
+                const float f = __builtin_bit_cast(float, now.sz[g] & ~15u);
 #pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    const float f = __builtin_bit_cast(float, now.sz[t][g] & ~15u);
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) {
-                        float v = (float)acc[u][t][j];
-                        if constexpr (GS) v *= xs[j >> 2][j & 3];
-                        total[u][t][j] = __builtin_fmaf(f, v, total[u][t][j]);
-                    }
-                    acc[u][t] = typename T::Acc{};
+                for (int j = 0; j < 16; ++j) {
+                    float v = (float)acc[u][j];
+                    if constexpr (GS) v *= xs[j >> 2][j & 3];
+                    total[u][j] = __builtin_fmaf(f, v, total[u][j]);
                 }
+                acc[u] = typename T::Acc{};
             }
             // (a second group's sums at the same time would not fit the registers)
 #pragma unroll
-            for (int u = 0; u < MT; ++u)
-#pragma unroll
-                for (int t = 0; t < NT; ++t) asm volatile("" : "+v"(total[u][t]));
+            for (int u = 0; u < MT; ++u) asm volatile("" : "+v"(total[u]));
         }
         if (more) commit(buf ^ 1);
     }
@@ -601,53 +524,46 @@ __global__ void __launch_bounds__(WM * WN * WK * 64, XT == FSCNN_F32 ? 1 : 2) ti
         const int mine = in_set * 64 + lane;
         if (wk > 0)
 #pragma unroll
-            for (int e = 0; e < MT * NT * 4; ++e) {
-                const q4f16 &f = total[e / 4 / NT][e / 4 % NT];
-                out[((wk - 1) * MT * NT * 4 + e) * kSet + mine] = q4f4{f[e % 4 * 4], f[e % 4 * 4 + 1], f[e % 4 * 4 + 2], f[e % 4 * 4 + 3]};
+            for (int e = 0; e < MT * 4; ++e) {
+                const q4f16 &f = total[e / 4];
+                out[((wk - 1) * MT * 4 + e) * kSet + mine] = q4f4{f[e % 4 * 4], f[e % 4 * 4 + 1], f[e % 4 * 4 + 2], f[e % 4 * 4 + 3]};
             }
         __syncthreads();
         if (wk == 0)
 #pragma unroll
-            for (int e = 0; e < MT * NT * 4; ++e)
+            for (int e = 0; e < MT * 4; ++e)
 #pragma unroll
                 for (int k = 0; k < WK - 1; ++k) {
-                    const q4f4 f = out[(k * MT * NT * 4 + e) * kSet + mine];
+                    const q4f4 f = out[(k * MT * 4 + e) * kSet + mine];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) total[e / 4 / NT][e / 4 % NT][e % 4 * 4 + i] += f[i];
+                    for (int i = 0; i < 4; ++i) total[e / 4][e % 4 * 4 + i] += f[i];
                 }
     }
     if (gridDim.y > 1) {
-        if (wk == 0)
+        const int k = n0 + (lane & 31);
+        if (wk == 0 && k < a.K)
 #pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                const int k = n0 + 32 * t + (lane & 31);
-                if (k < a.K)
+            for (int u = 0; u < MT; ++u)
 #pragma unroll
-                    for (int u = 0; u < MT; ++u)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const int m = m0 + wm * (32 * MT) + u * 32 + 8 * (i >> 2) + 4 * half + (i & 3);
-                            if (m < a.M) a.sums[((long long)blockIdx.y * a.M + m) * (a.tiles * 16LL) + k] = total[u][t][i];
-                        }
-            }
+                for (int i = 0; i < 16; ++i) {
+                    const int m = m0 + u * 32 + 8 * (i >> 2) + 4 * half + (i & 3);
+                    if (m < a.M) a.sums[((long long)blockIdx.y * a.M + m) * (a.tiles * 16LL) + k] = total[u][i];
+                }
         return;
     }
-    // 32 rows of every wave after the other by way of LDS, so that a lane stores 16 bytes of a row of y
+    // 32 rows after the other by way of LDS, so that a lane stores 16 bytes of a row of y
     float *const area = reinterpret_cast<float *>(lds);
-    const int cols0 = n0 - wn * (32 * NT);
+    const int cols0 = n0 - in_set * 32;
     const auto put = [&](int u) {
         if (wk == 0)
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    area[(u & 1) * kArea + (wm * 32 + 8 * (i >> 2) + 4 * half + (i & 3)) * kPitch + wn * (32 * NT) + t * 32 + (lane & 31)] = total[u][t][i];
+            for (int i = 0; i < 16; ++i) area[(u & 1) * kArea + (8 * (i >> 2) + 4 * half + (i & 3)) * kPitch + in_set * 32 + (lane & 31)] = total[u][i];
     };
     const auto store = [&](int u, auto type) {
         using E = typename Elem<decltype(type)::value>::type;
-        constexpr int kV = 16 / (int)sizeof(E), kRow = 32 * NT * WN / kV;   // outputs of a thread; threads of a row
-        for (int at = threadIdx.x; at < 32 * WM * kRow; at += kSet * WK) {
-            const int r = at / kRow, c = at % kRow * kV, m = m0 + (r >> 5) * (32 * MT) + u * 32 + (r & 31), k = cols0 + c;
+        constexpr int kV = 16 / (int)sizeof(E), kRow = 32 * WN / kV;   // outputs of a thread; threads of a row
+        for (int at = threadIdx.x; at < 32 * kRow; at += kSet * WK) {
+            const int r = at / kRow, c = at % kRow * kV, m = m0 + u * 32 + r, k = cols0 + c;
             if (m >= a.M || k >= a.K) continue;
             const float *f = area + (u & 1) * kArea + r * kPitch + c;
             const float xs = kInt && !GS ? a.x_scale[m] : 1.0f;
@@ -677,49 +593,47 @@ __global__ void __launch_bounds__(WM * WN * WK * 64, XT == FSCNN_F32 ? 1 : 2) ti
     }
 }
 
-template <int XT, int NT, int MT, int W> hipError_t launch_rows(const Q4Args &a, hipStream_t st)
+template <int XT, int W> hipError_t launch_rows(const Q4Args &a, hipStream_t st)
 {
-    const long long gx = (a.tiles + NT - 1) / NT, gy = ((long long)a.M + 16 * MT - 1) / (16 * MT);
-    if (gx * W * 64 > 0xffffffffLL || gy > 65535) return hipErrorInvalidValue;
-    const dim3 grid((unsigned)gx, (unsigned)gy), block(W * 64);
-    if (a.steps == 1) hipLaunchKernelGGL((rows_kernel<XT, NT, MT, W, 1>), grid, block, 0, st, a);
-    else if (a.steps == 2) hipLaunchKernelGGL((rows_kernel<XT, NT, MT, W, 2>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((rows_kernel<XT, NT, MT, W, 4>), grid, block, 0, st, a);
+    if (a.M > 16 || a.tiles * (W * 64LL) > 0xffffffffLL) return hipErrorInvalidValue;
+    const dim3 grid(a.tiles), block(W * 64);
+    if (a.steps == 1) hipLaunchKernelGGL((rows_kernel<XT, W, 1>), grid, block, 0, st, a);
+    else if (a.steps == 2) hipLaunchKernelGGL((rows_kernel<XT, W, 2>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((rows_kernel<XT, W, 4>), grid, block, 0, st, a);
     return hipGetLastError();
 }
 
-template <int XT, int NT, int W> hipError_t launch_staged(const Q4Args &a, hipStream_t st)
+template <int XT, int W> hipError_t launch_staged(const Q4Args &a, hipStream_t st)
 {
     constexpr int kBytes = XT == FSCNN_I8 ? 1 : 2, kMost = 144 << 10, kTurn = W * kQ4Block;
     const int rows = a.M * XOp<XT>::kParts;
-    const long long grid = (a.tiles + NT - 1) / NT;
-    if (rows > 16 || grid * W * 64 > 0xffffffffLL) return hipErrorInvalidValue;
+    if (rows > 16 || a.tiles * (W * 64LL) > 0xffffffffLL) return hipErrorInvalidValue;
     // as many columns in LDS as leave room for a second work-group where there is one for a CU
-    const int room = grid > 256 ? kMost / 2 : kMost, fit = (room / rows - 16) / kBytes / kTurn * kTurn, all = a.blocks * kQ4Block;
-    const int cols = all < fit ? all : fit, bytes = rows * (cols * kBytes + 16), sums = W * NT * 1024;
+    const int room = a.tiles > 256 ? kMost / 2 : kMost, fit = (room / rows - 16) / kBytes / kTurn * kTurn, all = a.blocks * kQ4Block;
+    const int cols = all < fit ? all : fit, bytes = rows * (cols * kBytes + 16), sums = W * 1024;
     static_assert(16 * (kTurn * kBytes + 16) <= kMost / 2, "a turn of 16 rows fits");
     auto launch = [&](auto kernel) {
         static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, kMost);
         if (attr != hipSuccess) return attr;
-        hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(W * 64), bytes > sums ? bytes : sums, st, a, cols);
+        hipLaunchKernelGGL(kernel, dim3(a.tiles), dim3(W * 64), bytes > sums ? bytes : sums, st, a, cols);
         return hipGetLastError();
     };
-    if (a.steps == 1) return launch(&staged_kernel<XT, NT, W, 1>);
-    if (a.steps == 2) return launch(&staged_kernel<XT, NT, W, 2>);
-    return launch(&staged_kernel<XT, NT, W, 4>);
+    if (a.steps == 1) return launch(&staged_kernel<XT, W, 1>);
+    if (a.steps == 2) return launch(&staged_kernel<XT, W, 2>);
+    return launch(&staged_kernel<XT, W, 4>);
 }
 
-template <int XT, int MT, int NT, int WM, int WN, int WK, bool DMA, bool GS> hipError_t launch_tiles(Q4Args a, int parts, hipStream_t st)
+template <int XT, int MT, int WN, int WK, bool DMA, bool GS> hipError_t launch_tiles(Q4Args a, int parts, hipStream_t st)
 {
-    constexpr int rows = 32 * MT * WM, threads = WM * WN * WK * 64;
-    const long long mt = ((long long)a.M + rows - 1) / rows, nt = (a.K + 32LL * NT * WN - 1) / (32 * NT * WN);
+    constexpr int rows = 32 * MT, threads = WN * WK * 64;
+    const long long mt = ((long long)a.M + rows - 1) / rows, nt = (a.K + 32LL * WN - 1) / (32 * WN);
     if (mt * nt * threads > 0xffffffffLL || 8 * nt > 0x7fffffffLL) return hipErrorInvalidValue;
     a.mt = (int)mt;
     a.nt = (int)nt;
     const dim3 grid((unsigned)(mt * nt), parts), block(threads);
-    if (a.steps == 1) hipLaunchKernelGGL((tile_kernel<XT, MT, NT, WM, WN, WK, 1, DMA, GS>), grid, block, 0, st, a);
-    else if (a.steps == 2) hipLaunchKernelGGL((tile_kernel<XT, MT, NT, WM, WN, WK, 2, DMA, GS>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((tile_kernel<XT, MT, NT, WM, WN, WK, 4, DMA, GS>), grid, block, 0, st, a);
+    if (a.steps == 1) hipLaunchKernelGGL((tile_kernel<XT, MT, WN, WK, 1, DMA, GS>), grid, block, 0, st, a);
+    else if (a.steps == 2) hipLaunchKernelGGL((tile_kernel<XT, MT, WN, WK, 2, DMA, GS>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((tile_kernel<XT, MT, WN, WK, 4, DMA, GS>), grid, block, 0, st, a);
     return hipGetLastError();
 }
 
@@ -737,15 +651,15 @@ struct TileCost {
     }
 };
 
-template <int XT, int MT, int NT, int WM, int WN, int WK> hipError_t launch_tiles(const Q4Args &a, hipStream_t st)
+template <int XT, int MT, int WN, int WK> hipError_t launch_tiles(const Q4Args &a, hipStream_t st)
 {
-    constexpr int rows = 32 * MT * WM;
+    constexpr int rows = 32 * MT;
     const bool dma = dma_serves(a, rows);
     if constexpr (XT == FSCNN_I8) {
         if (a.x_cols > 1)
-            return dma ? launch_tiles<XT, MT, NT, WM, WN, WK, true, true>(a, 1, st) : launch_tiles<XT, 2, 1, 1, 4, 1, false, true>(a, 1, st);
+            return dma ? launch_tiles<XT, MT, WN, WK, true, true>(a, 1, st) : launch_tiles<XT, 2, 4, 1, false, true>(a, 1, st);
     }
-    return dma ? launch_tiles<XT, MT, NT, WM, WN, WK, true, false>(a, 1, st) : launch_tiles<XT, 2, 1, 1, 4, 1, false, false>(a, 1, st);
+    return dma ? launch_tiles<XT, MT, WN, WK, true, false>(a, 1, st) : launch_tiles<XT, 2, 4, 1, false, false>(a, 1, st);
 }
 
 // x in 16 or 8 bits.  The fastest of five shapes of tile_kernel by what launches of them take (fitted to 1 to 4096 rows, 1024 to 16384 columns, 1024 to
@@ -771,16 +685,16 @@ template <int XT> hipError_t launch_narrow(const Q4Args &a, hipStream_t st)
         const int n = (a.tiles + 255) / 256;
         const bool deep = a.blocks >= 64 && n == 1;
         if (a.M <= 4 || 2.9f + n * (a.blocks / 32.0f) * (0.95f + 0.13f * a.M) <= us) {
-            if (a.M > 2) return deep ? launch_staged<XT, 1, 16>(a, st) : launch_staged<XT, 1, 8>(a, st);
-            return deep ? launch_rows<XT, 1, 1, 16>(a, st) : launch_rows<XT, 1, 1, 8>(a, st);
+            if (a.M > 2) return deep ? launch_staged<XT, 16>(a, st) : launch_staged<XT, 8>(a, st);
+            return deep ? launch_rows<XT, 16>(a, st) : launch_rows<XT, 8>(a, st);
         }
     }
     switch (best) {
-        case 0: return launch_tiles<XT, 1, 1, 1, 1, 8>(a, st);
-        case 1: return launch_tiles<XT, 1, 1, 1, 2, 4>(a, st);
-        case 2: return launch_tiles<XT, 2, 1, 1, 4, 2>(a, st);
-        case 3: return launch_tiles<XT, 2, 1, 1, 4, 1>(a, st);
-        default: return launch_tiles<XT, 4, 1, 1, 4, 1>(a, st);
+        case 0: return launch_tiles<XT, 1, 1, 8>(a, st);
+        case 1: return launch_tiles<XT, 1, 2, 4>(a, st);
+        case 2: return launch_tiles<XT, 2, 4, 2>(a, st);
+        case 3: return launch_tiles<XT, 2, 4, 1>(a, st);
+        default: return launch_tiles<XT, 4, 4, 1>(a, st);
     }
 }
 
