@@ -7,8 +7,9 @@
 // at thread i mod TH, and issues all loads of its row before it uses the first.  A group of 32 to 128 columns lies in 4 to 32 adjacent
 // lanes.  Measured: 16384 rows of 4096 in bf16 with residual 93 us, 5.8 TB/s, in 8 bits 87; 2^19 rows of 128 91 us (with a wave a row 248);
 // one row of 4096 3.4 us, of which a launch is most.
-// Codes are formed in 32 bits: six in a million are next to the border between two and may be the other one.  In 64 bits none was, for 10 to 25% more
-// time (2^14 rows of 4096: 107 us).
+// Codes are formed in 32 bits: 2 to 7 in a million elements are so near the border between two codes that they get the other one (with
+// elementary operations in 32 bits 1 to 5).  In 64 bits none was for fp32 rows, for 10 to 25% more time; 16-bit rows have exact ties
+// that no precision settles.
 #include <type_traits>
 
 #include "internal.h"
