@@ -662,21 +662,23 @@ template <int XT, int MT, int WN, int WK> hipError_t launch_tiles(const Q4Args &
     return dma ? launch_tiles<XT, MT, WN, WK, true, false>(a, 1, st) : launch_tiles<XT, 2, 4, 1, false, false>(a, 1, st);
 }
 
-// x in 16 or 8 bits.  The fastest of five shapes of tile_kernel by what launches of them take (fitted to 1 to 4096 rows, 1024 to 16384 columns, 1024 to
-// 12288 weight rows, within 15 %): many sets where few work-groups are there, whose sums through LDS cost more than they bring
-// where they are many (bf16, 4096 -> 4096: 64 rows of x 9.3 us with 32 x 32 in 8 sets, 28 with 64 x 128 in one; 1024 rows 117 and 45).  Rows of x that
+// x in 16 or 8 bits.  The fastest of seven shapes of tile_kernel, in 8 bits five, by what launches of them take (fitted to 1 to 4096 rows, 1024 to
+// 16384 columns, 1024 to 12288 weight rows, within 15 %; in 16 bits the choice is 0.4 % behind the fastest in the mean, in 8 bits 2.4): many sets
+// where few work-groups are there, whose sums through LDS cost more than they bring where they are many (bf16, 4096 -> 4096: 64 rows of x 9.3 us
+// with 32 x 32 in 8 sets, 28 with 64 x 128 in one; 1024 rows 117 and 45), and the shape whose work-groups leave the fewest CUs idle (200 rows
+// 17.4 us with 64 x 64 in 4 sets, 19.4 with the best of the others; 700 rows 33.3 with 96 x 128 in 2 sets and 39.2).  Rows of x that
 // are not 16 bytes aligned come by way of registers and have one shape.  Up to 16 rows also staged_kernel and, for one or two rows, whose operand is
 // not worth a barrier, rows_kernel (bf16, 4096 -> 4096: one row 3.7 us, 4.1 staged; 8 rows 5.5 and 4.9).  Sixteen waves where a wave of
 // eight had eight blocks or more (one row of 16384: 8.3 us, 10.3 with eight; of 4096: 3.9 and 3.7).
 template <int XT> hipError_t launch_narrow(const Q4Args &a, hipStream_t st)
 {
     constexpr bool kInt = XT == FSCNN_I8;
-    constexpr TileCost kTiles[5] = {{32, 32, 8, kInt ? 0.68f : 1.3f, kInt ? 0.8f : 1.55f}, {32, 64, 4, kInt ? 0.6f : 1.0f, kInt ? 0.6f : 0.93f},
-                                    {64, 128, 2, kInt ? 0.8f : 1.3f, kInt ? 0.79f : 1.42f}, {64, 128, 1, kInt ? 0.52f : 0.8f, kInt ? 0.41f : 0.62f},
-                                    {128, 128, 1, kInt ? 0.9f : 1.25f, kInt ? 0.72f : 1.08f}};
+    constexpr TileCost kTiles[7] = {{32, 32, 8, kInt ? 0.68f : 1.3f, kInt ? 0.8f : 1.55f}, {32, 64, 4, kInt ? 0.6f : 1.0f, kInt ? 0.6f : 0.93f},
+                                    {64, 128, 2, kInt ? 0.8f : 1.3f, kInt ? 0.79f : 1.2f}, {64, 128, 1, kInt ? 0.52f : 0.8f, kInt ? 0.41f : 0.62f},
+                                    {128, 128, 1, kInt ? 0.9f : 1.25f, kInt ? 0.72f : 1.08f}, {64, 64, 4, 1.6f, 1.72f}, {96, 128, 2, 1.65f, 1.78f}};
     int best = 0;
     float us = kTiles[0].us(a);
-    for (int i = 1; i < 5; ++i)
+    for (int i = 1; i < (kInt ? 5 : 7); ++i)
         if (const float t = kTiles[i].us(a); t < us) {
             us = t;
             best = i;
@@ -694,6 +696,8 @@ template <int XT> hipError_t launch_narrow(const Q4Args &a, hipStream_t st)
         case 1: return launch_tiles<XT, 1, 2, 4>(a, st);
         case 2: return launch_tiles<XT, 2, 4, 2>(a, st);
         case 3: return launch_tiles<XT, 2, 4, 1>(a, st);
+        case 5: if constexpr (!kInt) return launch_tiles<XT, 2, 2, 4>(a, st);
+        case 6: if constexpr (!kInt) return launch_tiles<XT, 3, 4, 2>(a, st);
         default: return launch_tiles<XT, 4, 4, 1>(a, st);
     }
 }
