@@ -7,17 +7,21 @@ namespace {
 
 constexpr int kQ4LaunchRows = 1 << 18;
 
-// What the work-groups that divide the columns have left, added in their order; a thread an output
-__global__ void __launch_bounds__(256) join_kernel(const Q4Args a, int parts)
+// What the P work-groups that divide the columns have left, added in their order; four outputs a thread, all loads on their way together
+template <int P> __global__ void __launch_bounds__(64) join_kernel(const Q4Args a)
 {
-    const int k = blockIdx.x * 256 + threadIdx.x;
+    const int k = (blockIdx.x * 64 + threadIdx.x) * 4;
     if (k >= a.K) return;
     const long long pitch = a.tiles * 16LL;
-    const float bias = a.bias ? a.bias[k] : 0.0f;
     for (int m = blockIdx.y; m < a.M; m += gridDim.y) {
-        float v = a.sums[m * pitch + k];
-        for (int p = 1; p < parts; ++p) v += a.sums[((long long)p * a.M + m) * pitch + k];
-        store_output(a, m, k, v, bias);
+        q4f4 v[P];
+#pragma unroll
+        for (int p = 0; p < P; ++p) __builtin_memcpy(&v[p], a.sums + (((long long)p * a.M + m) * pitch + k), 16);
+#pragma unroll
+        for (int p = 1; p < P; ++p) v[0] += v[p];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (k + i < a.K) store_output(a, m, k + i, v[0][i], a.bias ? a.bias[k + i] : 0.0f);
     }
 }
 
@@ -52,7 +56,11 @@ hipError_t launch_linear_q4(const fscnn_q4 *q, const void *x, int x_type, long l
         }
         if (e != hipSuccess) return e;
         if (parts > 1) {
-            hipLaunchKernelGGL(join_kernel, dim3((unsigned)((a.K + 255) / 256), a.M), dim3(256), 0, st, a, parts);
+            const dim3 grid((unsigned)((a.K + 255) / 256), a.M < 65535 ? a.M : 65535);
+            if (parts == 2) hipLaunchKernelGGL(join_kernel<2>, grid, dim3(64), 0, st, a);
+            else if (parts == 4) hipLaunchKernelGGL(join_kernel<4>, grid, dim3(64), 0, st, a);
+            else if (parts == 8) hipLaunchKernelGGL(join_kernel<8>, grid, dim3(64), 0, st, a);
+            else hipLaunchKernelGGL(join_kernel<16>, grid, dim3(64), 0, st, a);
             e = hipGetLastError();
             if (e != hipSuccess) return e;
         }

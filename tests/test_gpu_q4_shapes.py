@@ -50,7 +50,7 @@ def test_scratch(F, m, c, k):  # noqa: F811
     L.fscnn_linear_q4_workspace.restype = ll
     need = L.fscnn_linear_q4_workspace(h.handle, 0, m)
     assert need >= 0 and need % 4 == 0
-    ws = torch.full((need // 4 + 64,), 7.0, device="cuda")
+    ws = torch.full((need // 4 + 65,), 7.0, device="cuda")[1:]      # (4 bytes aligned, no more)
     for size in (need, need - 4, 4, 0):
         y = torch.zeros(m, k, device="cuda")
         st = L.fscnn_linear_q4(h.handle, ctypes.c_void_p(x.data_ptr()), 0, ll(c), None, 1, m, c, None, ctypes.c_float(1.0), ctypes.c_void_p(y.data_ptr()), 0, ll(k),
