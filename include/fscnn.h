@@ -468,8 +468,8 @@ fscnn_status_t fscnn_q4_import(const unsigned char *codes_dev, const void *scale
 /* Any output pointer may be NULL; *zeros: whether the handle has zero points of its own. */
 fscnn_status_t fscnn_q4_info(const fscnn_q4_t *q, int *K, int *C, int *group, int *zeros, fscnn_dtype_t *scale_type);
 
-/* Codes, scales and zero points (NULL, or 8 where the handle has none of its own) as fscnn_q4_import takes them, copied to HOST buffers; the high bits of an odd row's
- * last byte are 0.  Synchronous. */
+/* Codes, scales and zero points (zeros_host may be NULL; 8 where the handle has none of its own) as fscnn_q4_import takes them, copied to HOST
+ * buffers; the high bits of an odd row's last byte are 0.  Synchronous. */
 fscnn_status_t fscnn_q4_export(const fscnn_q4_t *q, unsigned char *codes_host, void *scales_host, unsigned char *zeros_host);
 fscnn_status_t fscnn_q4_destroy(fscnn_q4_t *q);
 
@@ -477,8 +477,8 @@ fscnn_status_t fscnn_q4_destroy(fscnn_q4_t *q);
  * x_dev: M rows of C elements of x_type, rows ldx >= C elements apart; y_dev: M rows of K elements of y_type (F32, F16, BF16), rows
  * ldy >= K elements apart, what lies between them is left as it is; both aligned to their type (16-byte aligned rows are read faster).
  * bias_dev: K floats or NULL.  negative_slope in [0, 1]: 1 no activation, 0 ReLU, between them LeakyReLU; else FSCNN_ERR_SHAPE.
- * x_type F32, F16, BF16: x_scale_dev NULL; products are formed with the codes as they are, sums are held in fp32 and every group's is
- * multiplied by its scale in fp32; y is rounded once.  (F32: x enters as three bfloat16 parts, their sum within 2^-24 of it.)
+ * x_type F32, F16, BF16: x_scale_dev NULL; products are formed with the codes, or with code - zero (both exact), sums are held in fp32 and every group's
+ * is multiplied by its scale in fp32; y is rounded once.  (F32: x enters as three bfloat16 parts, their sum within 2^-24 of it.)
  * x_type I8: x[m][c] stands for x_dev[m][c] * x_scale, x_scale_dev M x x_scale_cols floats, one for the row (x_scale_cols 1) or one for
  * each group of the weights (ceil(C/group)); a group's sum is exact in 32-bit integers.
  * An x that is not finite meets every weight of its row, zeros among them; other rows are not touched by it.  M == 0 is no work (pointers

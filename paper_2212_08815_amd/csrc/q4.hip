@@ -54,10 +54,18 @@ __global__ void __launch_bounds__(256) import_kernel(const Shape p, const unsign
         zero &= 15;
     }
     const long long pitch = ((long long)p.C + 1) / 2;
-    for (int j = 0; j < 8; ++j) {
-        uint32_t code = live ? zero : 0;
-        if (live && col + j < p.C) code = codes[row * pitch + ((col + j) >> 1)] >> (4 * (j & 1)) & 15;
-        w |= code << nibble_of(j);
+    if (live && col + 8 <= p.C) {
+        uint32_t in;                          // column j in bits 4 j: the first four go to the low halves of the bytes, the others to the high ones
+        __builtin_memcpy(&in, codes + (row * pitch + (col >> 1)), 4);
+        const uint32_t lo = in & 0xffff, hi = in >> 16;
+        const auto spread = [](uint32_t v) {
+            v = (v | v << 8) & 0x00ff00ff;
+            return (v | v << 4) & 0x0f0f0f0f;
+        };
+        w = spread(lo) | spread(hi) << 4;
+    } else if (live) {
+        for (int j = 0; j < 8; ++j)
+            w |= (col + j < p.C ? codes[row * pitch + ((col + j) >> 1)] >> (4 * (j & 1)) & 15 : zero) << nibble_of(j);
     }
     out[i] = w;
     if (col % p.group == 0) {

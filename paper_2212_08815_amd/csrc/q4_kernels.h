@@ -476,14 +476,16 @@ __global__ void __launch_bounds__(WN * WK * 64, XT == FSCNN_F32 ? 1 : 2) tile_ke
         now = next;
         // step st of the block: the weights' operand
         auto decode = [&](int st) {
-            const typename X::Zero z = X::zero(now.sz[st / kStepsOfGroup]);
-            if constexpr (kInt) {
-                const u2v w0 = X::weights(now.w[0][st], z), w1 = X::weights(now.w[1][st], z);
-                return u4v{w0[0], w0[1], w1[0], w1[1]};
-            } else if constexpr (kSumX) {
+            if constexpr (kSumX) {
                 return X::codes(now.w[st & 1][st >> 1]);
             } else {
-                return X::weights(now.w[st & 1][st >> 1], z);
+                const typename X::Zero z = X::zero(now.sz[st / kStepsOfGroup]);
+                if constexpr (kInt) {
+                    const u2v w0 = X::weights(now.w[0][st], z), w1 = X::weights(now.w[1][st], z);
+                    return u4v{w0[0], w0[1], w1[0], w1[1]};
+                } else {
+                    return X::weights(now.w[st & 1][st >> 1], z);
+                }
             }
         };
         const u4v *from_lds = set + buf * kBuf + row0 * kCh;

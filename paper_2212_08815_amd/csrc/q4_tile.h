@@ -120,9 +120,6 @@ template <> struct XOp<FSCNN_F32> {
         }
     }
     __device__ static Op codes(uint32_t w) { return XOp<FSCNN_BF16>::codes(w); }
-    using Zero = float;
-    __device__ static Zero zero(uint32_t word) { return XOp<FSCNN_BF16>::zero(word); }
-    __device__ static Op weights(uint32_t w, Zero z) { return XOp<FSCNN_BF16>::weights(w, z); }
     __device__ static Op ones() { return XOp<FSCNN_BF16>::ones(); }
     __device__ static Acc mfma(const Op &a, const Op &b, const Acc &c) { return XOp<FSCNN_BF16>::mfma(a, b, c); }
 };
