@@ -115,12 +115,6 @@ template <int XT, int PARTS, int W> __device__ inline void store_sums(const Q4Ar
     }
 }
 
-// The value of another lane of the row of 16
-template <int CTRL> __device__ inline float lane_swapped(float v)
-{
-    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 15, 15, true));
-}
-
 // 16 rows of weights, W waves
 template <int XT, int W, int STEPS> __global__ void __launch_bounds__(W * 64) rows_kernel(const Q4Args a)
 {
@@ -155,14 +149,16 @@ template <int XT, int W, int STEPS> __global__ void __launch_bounds__(W * 64) ro
             typename X::Op op[X::kParts];
             X::parts(raw[s], op);
             if constexpr (decltype(has)::value) load_x(then, s, std::false_type{});
-            const typename X::Op q = X::codes(v.w[s]);
+            if constexpr (X::kParts > 1) {    // (a product with ones costs more here than to subtract zero points, and the parts' sums lose a digit)
+                const typename X::Op q = X::weights(v.w[s], X::zero(v.sz[s / STEPS]));
 #pragma unroll
-            for (int p = 0; p < X::kParts; ++p) {
-                sum = X::mfma(op[p], X::ones(), sum);
-                acc = X::mfma(op[p], q, acc);
+                for (int p = 0; p < X::kParts; ++p) acc = X::mfma(op[p], q, acc);
+            } else {
+                sum = X::mfma(op[0], X::ones(), sum);
+                acc = X::mfma(op[0], X::codes(v.w[s]), acc);
             }
             if ((s + 1) % STEPS == 0) {       // the group's end
-                total = add_group<XT>(xs[s / STEPS], v.sz[s / STEPS], acc, sum, total);
+                total = add_group<XT>(xs[s / STEPS], X::kParts > 1 ? v.sz[s / STEPS] & ~15u : v.sz[s / STEPS], acc, sum, total);
                 acc = sum = typename X::Acc{};
                 // (a second group's sums at the same time would take more registers)
                 asm volatile("" : "+v"(total));
@@ -329,10 +325,7 @@ __global__ void __launch_bounds__(WN * WK * 64, XT == FSCNN_F32 ? 1 : 2) tile_ke
     constexpr int kSteps = kInt ? 4 : 8, kStepsOfGroup = kSteps / kGroups;   // products of a block, of a group
     constexpr int kPer = kRows * kCh / kSet;              // chunks a thread brings
     constexpr int kBuf = kRows * kCh * kParts;            // chunks of a buffer
-    // in 32 bits codes go in as they are and the sums of x, which passes registers, take the zero points' share away: 12 instructions less a step
-    // for 16 more a group (32 rows of 25088 x 4096 28.3 us, with weights that have their zero points subtracted 30)
-    constexpr bool kSumX = XT == FSCNN_F32;
-    constexpr int kScales = GS || kSumX ? 2 * kGroups * kRows / 4 : 0;   // of x by row and group: its scales, or sums
+    constexpr int kScales = GS ? 2 * kGroups * kRows / 4 : 0;
     constexpr int kSums = (WK - 1) * kSet * MT * 4;  // in 16 bytes, at the end
     constexpr int kChunksOfSet = 2 * kBuf + kScales;
     static_assert(kPer * kSet == kRows * kCh, "a whole number of chunks a thread");
@@ -391,18 +384,6 @@ __global__ void __launch_bounds__(WN * WK * 64, XT == FSCNN_F32 ? 1 : 2) tile_ke
             X::parts(v.r[0], part);
 #pragma unroll
             for (int p = 0; p < kParts; ++p) to[p * kRows * kCh] = part[p];
-        }
-        if constexpr (kSumX) {
-            // 16 adjacent lanes hold a row's block, 4 STEPS of them a group (the swizzle keeps them together)
-            float f[8], sum;
-            __builtin_memcpy(f, &v.r[0], sizeof(f));
-            sum = ((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]));
-            sum += lane_swapped<0xb1>(sum);               // quad_perm 1 0 3 2
-            sum += lane_swapped<0x4e>(sum);               // quad_perm 2 3 0 1
-            if constexpr (STEPS >= 2) sum += lane_swapped<0x141>(sum);   // row_half_mirror
-            if constexpr (STEPS == 4) sum += lane_swapped<0x140>(sum);   // row_mirror
-            const int at = slot + i * 64, r = at / kCh, c = at % kCh ^ swizzle(r);
-            if (at % (4 * STEPS) == 0) set_scales[(buf * kGroups + c / (4 * STEPS)) * kRows + r] = sum;
         }
     };
     Chunk raw[DMA ? 1 : kPer];
@@ -476,16 +457,12 @@ __global__ void __launch_bounds__(WN * WK * 64, XT == FSCNN_F32 ? 1 : 2) tile_ke
         now = next;
         // step st of the block: the weights' operand
         auto decode = [&](int st) {
-            if constexpr (kSumX) {
-                return X::codes(now.w[st & 1][st >> 1]);
+            const typename X::Zero z = X::zero(now.sz[st / kStepsOfGroup]);
+            if constexpr (kInt) {
+                const u2v w0 = X::weights(now.w[0][st], z), w1 = X::weights(now.w[1][st], z);
+                return u4v{w0[0], w0[1], w1[0], w1[1]};
             } else {
-                const typename X::Zero z = X::zero(now.sz[st / kStepsOfGroup]);
-                if constexpr (kInt) {
-                    const u2v w0 = X::weights(now.w[0][st], z), w1 = X::weights(now.w[1][st], z);
-                    return u4v{w0[0], w0[1], w1[0], w1[1]};
-                } else {
-                    return X::weights(now.w[st & 1][st >> 1], z);
-                }
+                return X::weights(now.w[st & 1][st >> 1], z);
             }
         };
         const u4v *from_lds = set + buf * kBuf + row0 * kCh;
@@ -523,16 +500,15 @@ __global__ void __launch_bounds__(WN * WK * 64, XT == FSCNN_F32 ? 1 : 2) tile_ke
 #pragma unroll
             for (int u = 0; u < MT; ++u) {
                 q4f4 xs[4];
-                if constexpr (GS || kSumX) {
+                if constexpr (GS) {
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
                         xs[j] = *reinterpret_cast<const q4f4 *>(set_scales + (buf * kGroups + g) * kRows + u * 32 + 8 * j + 4 * half);
                 }
-                const float f = __builtin_bit_cast(float, now.sz[g] & ~15u), zero = (float)(now.sz[g] & 15);
+                const float f = __builtin_bit_cast(float, now.sz[g] & ~15u);
 #pragma unroll
                 for (int j = 0; j < 16; ++j) {
                     float v = (float)acc[u][j];
-                    if constexpr (kSumX) v = __builtin_fmaf(-zero, xs[j >> 2][j & 3], v);
                     if constexpr (GS) v *= xs[j >> 2][j & 3];
                     total[u][j] = __builtin_fmaf(f, v, total[u][j]);
                 }

@@ -125,3 +125,23 @@ def test_a_layer_captured(F, m):  # noqa: F811
         y2, out2 = layer()
         torch.cuda.synchronize()
         assert torch.equal(y, y2) and torch.equal(out, out2) and bool(y.any())
+
+
+@pytest.mark.parametrize("kind", ["relu", "positive"])
+@pytest.mark.parametrize("m", [1, 4, 8, 14, 40, 200])
+def test_precision_of_values_that_are_not_negative(F, m, kind):  # noqa: F811
+    """fp32 rows without negative values, whose sums with codes are far larger than with weights.  Per group 24 additions in the matrix cores (three
+    parts, eight steps), each off by at most a step of the sum so far, 2^-23 of it, if it cuts; 32 groups are added with half a step each.  Sums of
+    weights around zero grow like a root, their mean size on the way is 2/3 of the last one: (24 + 32 / 2) * 2/3 * 2^-23 = 27 * 2^-23 of the
+    result, in the mean over the outputs, had every addition erred to the same side; they do not."""
+    c, k = 4096, 512
+    g = rng(m)
+    wd = torch.randn(k, c, generator=g, device="cuda") / 64
+    h = F.q4_compress(wd, 128, True)
+    codes, scales, zeros = (t.cuda() for t in F.q4_export(h))
+    w = dense(torch.stack([codes & 15, codes >> 4], 2).view(k, -1), scales, zeros, 128)[0]
+    x = torch.randn(m, c, generator=g, device="cuda")
+    x = x.clamp(min=0) if kind == "relu" else x.abs() + 3
+    want = x.double() @ w.t()
+    got = F.linear_q4(h, x).double()
+    assert float((got - want).norm()) <= 27 * 2.0 ** -23 * float(want.norm())
