@@ -653,15 +653,11 @@ struct TileCost {
     }
 };
 
-template <int XT, int MT, int WN, int WK> hipError_t launch_tiles(const Q4Args &a, hipStream_t st)
+template <int XT, int MT, int WN, int WK, bool DMA> hipError_t launch_tiles(const Q4Args &a, hipStream_t st)
 {
-    constexpr int rows = 32 * MT;
-    const bool dma = dma_serves(a, rows);
-    if constexpr (XT == FSCNN_I8) {
-        if (a.x_cols > 1)
-            return dma ? launch_tiles<XT, MT, WN, WK, true, true>(a, 1, st) : launch_tiles<XT, 2, 4, 1, false, true>(a, 1, st);
-    }
-    return dma ? launch_tiles<XT, MT, WN, WK, true, false>(a, 1, st) : launch_tiles<XT, 2, 4, 1, false, false>(a, 1, st);
+    if constexpr (XT == FSCNN_I8)
+        if (a.x_cols > 1) return launch_tiles<XT, MT, WN, WK, DMA, true>(a, 1, st);
+    return launch_tiles<XT, MT, WN, WK, DMA, false>(a, 1, st);
 }
 
 // x in 16 or 8 bits.  The fastest of seven shapes of tile_kernel, in 8 bits five, by what launches of them take (fitted to 1 to 4096 rows, 1024 to
@@ -669,7 +665,8 @@ template <int XT, int MT, int WN, int WK> hipError_t launch_tiles(const Q4Args &
 // where few work-groups are there, whose sums through LDS cost more than they bring where they are many (bf16, 4096 -> 4096: 64 rows of x 9.3 us
 // with 32 x 32 in 8 sets, 28 with 64 x 128 in one; 1024 rows 117 and 45), and the shape whose work-groups leave the fewest CUs idle (200 rows
 // 17.4 us with 64 x 64 in 4 sets, 19.4 with the best of the others; 700 rows 33.3 with 96 x 128 in 2 sets and 39.2).  Rows of x that
-// are not 16 bytes aligned come by way of registers and have one shape.  Up to 16 rows also staged_kernel and, for one or two rows, whose operand is
+// are not 16 bytes aligned come by way of registers and have four shapes (fp16, 4097 -> 4096: 64 rows 15.4 us with 32 x 32 in 8 sets, 36 with
+// 64 x 128 in one; 2048 rows 407 and 94).  Up to 16 rows also staged_kernel and, for one or two rows, whose operand is
 // not worth a barrier, rows_kernel (bf16, 4096 -> 4096: one row 3.7 us, 4.1 staged; 8 rows 5.5 and 4.9).  Sixteen waves where a wave of
 // eight had eight blocks or more (one row of 16384: 8.3 us, 10.3 with eight; of 4096: 3.9 and 3.7).
 template <int XT> hipError_t launch_narrow(const Q4Args &a, hipStream_t st)
@@ -678,10 +675,13 @@ template <int XT> hipError_t launch_narrow(const Q4Args &a, hipStream_t st)
     constexpr TileCost kTiles[7] = {{32, 32, 8, kInt ? 0.68f : 1.3f, kInt ? 0.8f : 1.55f}, {32, 64, 4, kInt ? 0.6f : 1.0f, kInt ? 0.6f : 0.93f},
                                     {64, 128, 2, kInt ? 0.8f : 1.3f, kInt ? 0.79f : 1.2f}, {64, 128, 1, kInt ? 0.52f : 0.8f, kInt ? 0.41f : 0.62f},
                                     {128, 128, 1, kInt ? 0.9f : 1.25f, kInt ? 0.72f : 1.08f}, {64, 64, 4, 1.6f, 1.72f}, {96, 128, 2, 1.65f, 1.78f}};
+    constexpr TileCost kLoose[4] = {{32, 32, 8, kInt ? 1.5f : 2.1f, kInt ? 1.3f : 2.5f}, {32, 64, 4, kInt ? 1.05f : 1.28f, kInt ? 0.82f : 1.04f},
+                                    {64, 128, 2, kInt ? 1.26f : 1.54f, kInt ? 1.42f : 1.6f}, {64, 128, 1, kInt ? 0.8f : 1.0f, kInt ? 0.56f : 0.69f}};
+    const bool dma = dma_serves(a, 128);
     int best = 0;
-    float us = kTiles[0].us(a);
-    for (int i = 1; i < (kInt ? 5 : 7); ++i)
-        if (const float t = kTiles[i].us(a); t < us) {
+    float us = 0.0f;
+    for (int i = 0; i < (!dma ? 4 : kInt ? 5 : 7); ++i)
+        if (const float t = dma ? kTiles[i].us(a) : kLoose[i].us(a); i == 0 || t < us) {
             us = t;
             best = i;
         }
@@ -694,13 +694,13 @@ template <int XT> hipError_t launch_narrow(const Q4Args &a, hipStream_t st)
         }
     }
     switch (best) {
-        case 0: return launch_tiles<XT, 1, 1, 8>(a, st);
-        case 1: return launch_tiles<XT, 1, 2, 4>(a, st);
-        case 2: return launch_tiles<XT, 2, 4, 2>(a, st);
-        case 3: return launch_tiles<XT, 2, 4, 1>(a, st);
-        case 5: if constexpr (!kInt) return launch_tiles<XT, 2, 2, 4>(a, st);
-        case 6: if constexpr (!kInt) return launch_tiles<XT, 3, 4, 2>(a, st);
-        default: return launch_tiles<XT, 4, 4, 1>(a, st);
+        case 0: return dma ? launch_tiles<XT, 1, 1, 8, true>(a, st) : launch_tiles<XT, 1, 1, 8, false>(a, st);
+        case 1: return dma ? launch_tiles<XT, 1, 2, 4, true>(a, st) : launch_tiles<XT, 1, 2, 4, false>(a, st);
+        case 2: return dma ? launch_tiles<XT, 2, 4, 2, true>(a, st) : launch_tiles<XT, 2, 4, 2, false>(a, st);
+        case 3: return dma ? launch_tiles<XT, 2, 4, 1, true>(a, st) : launch_tiles<XT, 2, 4, 1, false>(a, st);
+        case 5: if constexpr (!kInt) return launch_tiles<XT, 2, 2, 4, true>(a, st);
+        case 6: if constexpr (!kInt) return launch_tiles<XT, 3, 4, 2, true>(a, st);
+        default: return launch_tiles<XT, 4, 4, 1, true>(a, st);
     }
 }
 
