@@ -1,6 +1,8 @@
 /*
  * fscnn.h -- C ABI of the MI355X (gfx950) sparse-filter / sparse-input 2-D
  * convolution library: the hot path of FSCNN (arXiv 2212.08815).
+ * Its last section: products with 4-bit weights, and the norm that feeds them
+ * (matrices of several types, aligned to their type, rows that may lie apart).
  *
  * Notation (paper -> here): input T_I (C_I x H_I x W_I) -> x[N,C,H,W], dense
  * NCHW fp32; filters T_F1..T_FN (C_F x H_F x W_F, C_F = C_I, C_O = N of the

@@ -10,10 +10,11 @@
 // while the next one is on its way there (16 bytes a lane, without registers where x is aligned); codes come from memory into registers a
 // block ahead.  WK sets may divide the blocks; their sums are added through LDS.  What a wave does per block (16 bits, MT = 4): 32 products of
 // 32 x 32 x 16, 1024 clocks of the matrix core, 19 vector instructions for every 8 codes a lane, 152, and 64 multiply-adds, since a
-// group's sum is multiplied by its scale in fp32; with addresses and staging 263.  The two hardly overlap, on one wave or on two
-// (counted: 4350 clocks of a SIMD per two such blocks, 2048 of products and 2100 of vector instructions), so what counts is how few of
-// the latter there are: hence 128 rows of x per decoded weight.  4096 rows of 4096 x 12288, bf16: 415 us, 0.99 PFLOP/s; without the
-// stores 375, without decoding 330.  Decoding for twice the rows at once, or a second block of codes ahead, brought nothing.
+// group's sum is multiplied by its scale in fp32; with addresses and staging 263.  So what counts is how few of the latter there are for a
+// product: hence 128 rows of x per decoded weight.  4096 rows of 4096 x 12288, bf16: 415 us, 0.99 PFLOP/s.  Matrix cores are busy 47 % of the
+// clocks there; decoding takes 13 %, scales 7, the rows' way to LDS 11, stores 10, LDS reads 4.  Decoding for twice the rows at once, codes
+// two blocks ahead, products and vector instructions interleaved by hand, and one barrier a block with the next block's first
+// operands read beside the last products brought 1 % or less, or lost.
 #pragma once
 #include <type_traits>
 
