@@ -145,3 +145,59 @@ def test_precision_of_values_that_are_not_negative(F, m, kind):  # noqa: F811
     want = x.double() @ w.t()
     got = F.linear_q4(h, x).double()
     assert float((got - want).norm()) <= 27 * 2.0 ** -23 * float(want.norm())
+
+
+@pytest.mark.parametrize("xt", TYPES, ids=["f32", "f16", "bf16", "i8"])
+@pytest.mark.parametrize("m", [1, 5, 12, 40])
+def test_the_longest_rows(F, m, xt):  # noqa: F811
+    """2^20 columns, the most there may be: sums stay below 2^22 (a random walk of 2^20 steps of at most 30)."""
+    h, x, xs, want = problem(F, m, 1 << 20, 20, xt, 128, True, 1)
+    assert float(want.abs().max()) < 2 ** 22
+    assert torch.equal(F.linear_q4(h, x, x_scale=xs, out_dtype=torch.float32).double(), want)
+
+
+def test_codes_at_any_byte(F):  # noqa: F811
+    g = rng(4)
+    for k, c in ((33, 129), (40, 1024), (17, 7), (20, 8)):
+        q, s, z = weights(g, k, c, 32, True)
+        p = packed(q)
+        want = F.q4_export(F.q4_import(p, s, z, group=32, c=c))
+        for off in (1, 2, 3):
+            buf = torch.full((p.numel() + off + 8,), 255, dtype=torch.uint8, device="cuda")
+            view = buf[off:off + p.numel()].view(p.shape)
+            view.copy_(p)
+            assert all(torch.equal(a, b) for a, b in zip(F.q4_export(F.q4_import(view, s, z, group=32, c=c)), want))
+
+
+def test_threads(F):  # noqa: F811
+    """Four threads, each on a stream of its own, with one set of weights: products with and without scratch, and the norm."""
+    import threading
+    g = rng(6)
+    d, k = 2048, 96
+    q, s, z = weights(g, k, d, 128, True)
+    h = F.q4_import(packed(q), s, z, group=128, c=d)
+    xs = [torch.randn(m, d, generator=g, device="cuda") for m in (1, 12, 60, 130)]
+    w = torch.ones(d, device="cuda")
+    layer = lambda x: (F.linear_q4(h, x), F.linear_q4(h, x.half()), F.rms_norm(x, w), *F.rms_norm_q8(x, w, group=64))
+    want = [layer(x) for x in xs]
+    torch.cuda.synchronize()
+    bad = []
+
+    def work(i):
+        try:
+            st = torch.cuda.Stream()
+            with torch.cuda.stream(st):
+                for _ in range(20):
+                    got = layer(xs[i])
+                    st.synchronize()
+                    if not all(torch.equal(a, b) for a, b in zip(got, want[i])):
+                        bad.append(i)
+        except Exception as e:
+            bad.append(e)
+
+    ts = [threading.Thread(target=work, args=(i,)) for i in range(4)]
+    for t in ts:
+        t.start()
+    for t in ts:
+        t.join()
+    assert not bad
