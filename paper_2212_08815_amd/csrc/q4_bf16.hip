@@ -3,9 +3,9 @@
 
 namespace fscnn {
 
-template <> hipError_t launch_q4_type<FSCNN_BF16>(const Q4Args &a, int, hipStream_t st)
+template <> hipError_t launch_q4_type<FSCNN_BF16>(const Q4Args &a, int parts, hipStream_t st)
 {
-    return launch_narrow<FSCNN_BF16>(a, st);
+    return launch_narrow<FSCNN_BF16>(a, parts, st);
 }
 
 }  // namespace fscnn

@@ -36,6 +36,9 @@ struct Q4Args {
     int mt, nt;                               // tile_kernel: tiles of the launch
 };
 
+// Columns divided over `parts` work-groups cost a second launch, and the sums' way to memory and back (us)
+inline double sums_us(double M, double tiles, int parts) { return parts > 1 ? 2.5 + parts * 1.28e-4 * M * tiles / 3 : 0; }
+
 // How 32-bit floats are served: kernel, and work-groups that divide the columns, at most `most` of them
 struct F32Choice {
     enum Kernel { kStaged, kRows, kTile32, kTile64 } kernel;
@@ -46,13 +49,13 @@ inline F32Choice f32_choice(long long tiles, int blocks, int M, int most)
     // (25088 -> 4096, one row: 14.1 us staged, 30 with a wave's own parts)
     if (M * XOp<FSCNN_F32>::kParts <= 16) return {F32Choice::kStaged, 1};
     // times of launches as TileCost has them; divided columns cost a launch and the sums' way to memory and back
-    const double wide = (double)((tiles + 15) / 16), sums = 1.28e-4 * M * tiles / 3;   // work-groups of a part of 32 or 64 rows; us a part
+    const double wide = (double)((tiles + 15) / 16);   // work-groups of a part of 32 or 64 rows
     F32Choice best = {F32Choice::kTile32, 1};
     double us = 1e30;
     for (int rows = 32; rows <= 64; rows *= 2)
         for (int p = 1; p <= most && p <= 16 && blocks / p >= 4; p *= 2) {
             const double n = __builtin_ceil(wide * ((M + rows - 1) / rows) * p / 256);
-            const double t = 4 + n * ((blocks + p - 1) / p) * (rows == 32 ? 1.45 : 2.65) + (p > 1 ? 2.5 + p * sums : 0);
+            const double t = 4 + n * ((blocks + p - 1) / p) * (rows == 32 ? 1.45 : 2.65) + sums_us(M, (double)tiles, p);
             if (t < us) {
                 us = t;
                 best = {rows == 32 ? F32Choice::kTile32 : F32Choice::kTile64, p};
@@ -550,7 +553,10 @@ __global__ void __launch_bounds__(WN * WK * 64, XT == FSCNN_F32 ? 1 : 2) tile_ke
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     const int m = m0 + u * 32 + 8 * (i >> 2) + 4 * half + (i & 3);
-                    if (m < a.M) a.sums[((long long)blockIdx.y * a.M + m) * (a.tiles * 16LL) + k] = total[u][i];
+                    if (m >= a.M) continue;
+                    float v = total[u][i];
+                    if constexpr (kInt && !GS) v *= a.x_scale[m];
+                    a.sums[((long long)blockIdx.y * a.M + m) * (a.tiles * 16LL) + k] = v;
                 }
         return;
     }
@@ -644,21 +650,22 @@ template <int XT, int MT, int WN, int WK, bool DMA, bool GS> hipError_t launch_t
 inline bool dma_serves(const Q4Args &a, int rows) { return !(((uintptr_t)a.x | (uintptr_t)a.ldx) & 15) && a.ldx * rows < 0x7fff0000LL; }
 
 // Time of a launch in us: 4 and, for every turn (a block a set of waves), `one` while a CU has a work-group, `many` times the work-groups of a CU beyond
+// that; `parts` work-groups divide the columns
 struct TileCost {
     int rows, cols, sets;
     float one, many;
-    float us(const Q4Args &a) const
+    double us(double M, double K, int blocks, int parts) const
     {
-        const double groups = (double)((a.M + rows - 1) / rows) * ((a.K + cols - 1) / cols), n = __builtin_ceil(groups / 256);
-        return 4 + (a.blocks + sets - 1) / sets * (n > 1 && many * (float)n > one ? many * (float)n : one);
+        const double groups = __builtin_ceil(M / rows) * __builtin_ceil(K / cols) * parts, n = __builtin_ceil(groups / 256);
+        return 4 + ((blocks + parts - 1) / parts + sets - 1) / sets * (n > 1 && many * n > one ? many * n : one);
     }
 };
 
-template <int XT, int MT, int WN, int WK, bool DMA> hipError_t launch_tiles(const Q4Args &a, hipStream_t st)
+template <int XT, int MT, int WN, int WK, bool DMA> hipError_t launch_tiles(const Q4Args &a, int parts, hipStream_t st)
 {
     if constexpr (XT == FSCNN_I8)
-        if (a.x_cols > 1) return launch_tiles<XT, MT, WN, WK, DMA, true>(a, 1, st);
-    return launch_tiles<XT, MT, WN, WK, DMA, false>(a, 1, st);
+        if (a.x_cols > 1) return launch_tiles<XT, MT, WN, WK, DMA, true>(a, parts, st);
+    return launch_tiles<XT, MT, WN, WK, DMA, false>(a, parts, st);
 }
 
 // x in 16 or 8 bits.  The fastest of seven shapes of tile_kernel, in 8 bits five, by what launches of them take (fitted to 1 to 4096 rows, 1024 to
@@ -670,7 +677,11 @@ template <int XT, int MT, int WN, int WK, bool DMA> hipError_t launch_tiles(cons
 // 64 x 128 in one; 2048 rows 407 and 94).  Up to 16 rows also staged_kernel and, for one or two rows, whose operand is
 // not worth a barrier, rows_kernel (bf16, 4096 -> 4096: one row 3.7 us, 4.1 staged; 8 rows 5.5 and 4.9).  Sixteen waves where a wave of
 // eight had eight blocks or more (one row of 16384: 8.3 us, 10.3 with eight; of 4096: 3.9 and 3.7).
-template <int XT> hipError_t launch_narrow(const Q4Args &a, hipStream_t st)
+struct NarrowChoice {
+    int shape;
+    double us;
+};
+template <int XT> NarrowChoice narrow_choice(double M, double K, int blocks, int parts, bool dma)
 {
     constexpr bool kInt = XT == FSCNN_I8;
     constexpr TileCost kTiles[7] = {{32, 32, 8, kInt ? 0.68f : 1.3f, kInt ? 0.8f : 1.55f}, {32, 64, 4, kInt ? 0.6f : 1.0f, kInt ? 0.6f : 0.93f},
@@ -678,30 +689,47 @@ template <int XT> hipError_t launch_narrow(const Q4Args &a, hipStream_t st)
                                     {128, 128, 1, kInt ? 0.9f : 1.25f, kInt ? 0.72f : 1.08f}, {64, 64, 4, 1.6f, 1.72f}, {96, 128, 2, 1.65f, 1.78f}};
     constexpr TileCost kLoose[4] = {{32, 32, 8, kInt ? 1.5f : 2.1f, kInt ? 1.3f : 2.5f}, {32, 64, 4, kInt ? 1.05f : 1.28f, kInt ? 0.82f : 1.04f},
                                     {64, 128, 2, kInt ? 1.26f : 1.54f, kInt ? 1.42f : 1.6f}, {64, 128, 1, kInt ? 0.8f : 1.0f, kInt ? 0.56f : 0.69f}};
-    const bool dma = dma_serves(a, 128);
-    int best = 0;
-    float us = 0.0f;
+    NarrowChoice best = {0, 1e30};
     for (int i = 0; i < (!dma ? 4 : kInt ? 5 : 7); ++i)
-        if (const float t = dma ? kTiles[i].us(a) : kLoose[i].us(a); i == 0 || t < us) {
+        if (const double t = (dma ? kTiles[i] : kLoose[i]).us(M, K, blocks, parts); t < best.us) best = {i, t};
+    return best;
+}
+
+// Work-groups that divide the columns of more than 16 rows of x, at most `most`: where few weight rows leave CUs without one (64 rows, 20000 -> 300:
+// bf16 29.6 us, 11.2 in 16 parts; 200 rows, 25088 -> 512 35.4 and 22.6 in 8; int8 19.6 and 12.3 in 8)
+template <int XT> int narrow_parts(double M, long long tiles, int K, int blocks, int most)
+{
+    int best = 1;
+    double us = narrow_choice<XT>(M, K, blocks, 1, true).us;
+    for (int p = 2; p <= most && p <= 16 && blocks / p >= 4; p *= 2)
+        if (const double t = narrow_choice<XT>(M, K, blocks, p, true).us + sums_us(M, (double)tiles, p); t < us) {
             us = t;
-            best = i;
+            best = p;
         }
-    if (a.M <= 16) {
+    return best;
+}
+
+template <int XT> hipError_t launch_narrow(const Q4Args &a, int parts, hipStream_t st)
+{
+    constexpr bool kInt = XT == FSCNN_I8;
+    const bool dma = dma_serves(a, 128);
+    const NarrowChoice best = narrow_choice<XT>(a.M, a.K, a.blocks, parts, dma);
+    if (a.M <= 16 && parts == 1) {
         const int n = (a.tiles + 255) / 256;
         const bool deep = a.blocks >= 64 && n == 1;
-        if (a.M <= 4 || 2.9f + n * (a.blocks / 32.0f) * (0.95f + 0.13f * a.M) <= us) {
+        if (a.M <= 4 || 2.9f + n * (a.blocks / 32.0f) * (0.95f + 0.13f * a.M) <= best.us) {
             if (a.M > 2) return deep ? launch_staged<XT, 16>(a, st) : launch_staged<XT, 8>(a, st);
             return deep ? launch_rows<XT, 16>(a, st) : launch_rows<XT, 8>(a, st);
         }
     }
-    switch (best) {
-        case 0: return dma ? launch_tiles<XT, 1, 1, 8, true>(a, st) : launch_tiles<XT, 1, 1, 8, false>(a, st);
-        case 1: return dma ? launch_tiles<XT, 1, 2, 4, true>(a, st) : launch_tiles<XT, 1, 2, 4, false>(a, st);
-        case 2: return dma ? launch_tiles<XT, 2, 4, 2, true>(a, st) : launch_tiles<XT, 2, 4, 2, false>(a, st);
-        case 3: return dma ? launch_tiles<XT, 2, 4, 1, true>(a, st) : launch_tiles<XT, 2, 4, 1, false>(a, st);
-        case 5: if constexpr (!kInt) return launch_tiles<XT, 2, 2, 4, true>(a, st);
-        case 6: if constexpr (!kInt) return launch_tiles<XT, 3, 4, 2, true>(a, st);
-        default: return launch_tiles<XT, 4, 4, 1, true>(a, st);
+    switch (best.shape) {
+        case 0: return dma ? launch_tiles<XT, 1, 1, 8, true>(a, parts, st) : launch_tiles<XT, 1, 1, 8, false>(a, parts, st);
+        case 1: return dma ? launch_tiles<XT, 1, 2, 4, true>(a, parts, st) : launch_tiles<XT, 1, 2, 4, false>(a, parts, st);
+        case 2: return dma ? launch_tiles<XT, 2, 4, 2, true>(a, parts, st) : launch_tiles<XT, 2, 4, 2, false>(a, parts, st);
+        case 3: return dma ? launch_tiles<XT, 2, 4, 1, true>(a, parts, st) : launch_tiles<XT, 2, 4, 1, false>(a, parts, st);
+        case 5: if constexpr (!kInt) return launch_tiles<XT, 2, 2, 4, true>(a, parts, st);
+        case 6: if constexpr (!kInt) return launch_tiles<XT, 3, 4, 2, true>(a, parts, st);
+        default: return launch_tiles<XT, 4, 4, 1, true>(a, parts, st);
     }
 }
 

@@ -31,9 +31,12 @@ int q4_parts(const fscnn_q4 *q, int x_type, int M)
 {
     // (a launch's rows of x: the sums' room is for one launch, and bounded)
     constexpr double kMostBytes = 64 << 20;
-    if (x_type != FSCNN_F32 || M <= 0 || M > kQ4LaunchRows) return 1;
-    const int most = (int)(kMostBytes / (64.0 * q4_tiles(q->K) * M));
-    return f32_choice(q4_tiles(q->K), (int)q4_blocks(q->C), M, most > 1 ? most : 1).parts;
+    if (M <= (x_type == FSCNN_F32 ? 0 : 16) || M > kQ4LaunchRows) return 1;
+    const long long tiles = q4_tiles(q->K);
+    const int blocks = (int)q4_blocks(q->C), most = (int)(kMostBytes / (64.0 * tiles * M));
+    if (x_type == FSCNN_F32) return f32_choice(tiles, blocks, M, most > 1 ? most : 1).parts;
+    if (x_type == FSCNN_I8) return narrow_parts<FSCNN_I8>(M, tiles, q->K, blocks, most);
+    return narrow_parts<FSCNN_BF16>(M, tiles, q->K, blocks, most);
 }
 
 hipError_t launch_linear_q4(const fscnn_q4 *q, const void *x, int x_type, long long ldx, const float *x_scale, int x_scale_cols, int M,

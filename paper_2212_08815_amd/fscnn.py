@@ -772,10 +772,10 @@ def linear_q4(q, x, bias=None, relu=False, leaky=None, out=None, out_dtype=None,
         slope = 0.0 if relu else 1.0
     native, h, xt = _nat or _native(), q.address, _DTYPES[x.dtype]
     ws, need = None, 0
-    if xt == F32:                            # (the only type that wants scratch)
+    if M > 16 or xt == F32:                  # (fewer rows of other types want no scratch)
         need = native.linear_q4_workspace(h, xt, M)
         if need > 0:
-            ws = x.new_empty(need // 4)
+            ws = x.new_empty(need // x.element_size())       # (need: bytes, a multiple of 64)
     st = native.linear_q4(h, x.data_ptr(), xt, ldx, scale, cols, M, C, b, slope, out.data_ptr(), _DTYPES[want], ldy, None if ws is None else ws.data_ptr(),
                           need, torch._C._cuda_getCurrentRawStream(dev))
     if st != OK:

@@ -58,6 +58,25 @@ def test_scratch(F, m, c, k):  # noqa: F811
         assert st == 0 and torch.equal(y.double(), want) and bool((ws[need // 4:] == 7).all())
 
 
+@pytest.mark.parametrize("rows", [0, 1], ids=["groups", "rows"])
+@pytest.mark.parametrize("xt", TYPES[1:], ids=["f16", "bf16", "i8"])
+@pytest.mark.parametrize("m,c,k", [(64, 20001, 300), (20, 9000, 512), (200, 8200, 250), (17, 4096, 256), (130, 1100, 40)])
+def test_scratch_of_narrow_rows(F, m, c, k, xt, rows):  # noqa: F811
+    """The same of rows in 16 and 8 bits, which have scales by group or by row."""
+    h, x, xs, want = problem(F, m, c, k, xt, 128, True, rows)
+    L, ll, t = F.lib(), ctypes.c_longlong, F._DTYPES[xt]
+    L.fscnn_linear_q4_workspace.restype = ll
+    need = L.fscnn_linear_q4_workspace(h.handle, t, m)
+    assert need >= 0 and need % 64 == 0
+    ws = torch.full((need // 4 + 65,), 7.0, device="cuda")[1:]
+    for size in (need, need - 4, 0):
+        y = torch.zeros(m, k, device="cuda")
+        st = L.fscnn_linear_q4(h.handle, ctypes.c_void_p(x.data_ptr()), t, ll(c), ctypes.c_void_p(xs.data_ptr()) if xs is not None else None,
+                               xs.numel() // m if xs is not None else 1, m, c, None, ctypes.c_float(1.0), ctypes.c_void_p(y.data_ptr()), 0, ll(k),
+                               ctypes.c_void_p(ws.data_ptr()) if size > 0 else None, ll(max(size, 0)), ctypes.c_void_p(torch.cuda.current_stream().cuda_stream))
+        assert st == 0 and torch.equal(y.double(), want) and bool((ws[need // 4:] == 7).all())
+
+
 @pytest.mark.parametrize("xt", TYPES, ids=["f32", "f16", "bf16", "i8"])
 def test_more_rows_than_a_launch_holds(F, xt):  # noqa: F811
     m, c, k = (1 << 18) + 77, 40, 24
@@ -201,3 +220,29 @@ def test_threads(F):  # noqa: F811
     for t in ts:
         t.join()
     assert not bad
+
+
+@pytest.mark.parametrize("xt", TYPES, ids=["f32", "f16", "bf16", "i8"])
+def test_the_binding_s_scratch_has_the_bytes_it_names(F, xt, monkeypatch):  # noqa: F811
+    """Nothing is launched: a stand-in for the native call looks at what it is handed."""
+    m, c, k = 64, 20000, 300
+    h = F.q4_import(torch.zeros(k, c // 2, dtype=torch.uint8, device="cuda"), torch.ones(k, (c + 127) // 128, dtype=torch.float16, device="cuda"))
+    native = F._native()
+    need = native.linear_q4_workspace(h.address, F._DTYPES[xt], m)
+    assert need > 0
+    seen = []
+
+    class Stand:
+        linear_q4_workspace = staticmethod(native.linear_q4_workspace)
+
+        @staticmethod
+        def linear_q4(*args):
+            seen.append((args[13], args[14], torch.cuda.memory_stats()["requested_bytes.all.allocated"]))
+            return 0
+
+    x, out = torch.zeros(m, c, dtype=xt, device="cuda"), torch.empty(m, k, dtype=torch.float32, device="cuda")
+    scale = torch.ones(m, device="cuda") if xt == torch.int8 else None
+    monkeypatch.setattr(F, "_nat", Stand)
+    before = torch.cuda.memory_stats()["requested_bytes.all.allocated"]
+    F.linear_q4(h, x, x_scale=scale, out=out)
+    assert len(seen) == 1 and seen[0][0] and seen[0][1] == need and seen[0][2] - before >= need
