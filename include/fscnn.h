@@ -483,7 +483,9 @@ fscnn_status_t fscnn_q4_destroy(fscnn_q4_t *q);
  * is multiplied by its scale in fp32; y is rounded once.  (F32: x enters as three bfloat16 parts, their sum within 2^-24 of it.)
  * x_type I8: x[m][c] stands for x_dev[m][c] * x_scale, x_scale_dev M x x_scale_cols floats, one for the row (x_scale_cols 1) or one for
  * each group of the weights (ceil(C/group)); a group's sum is exact in 32-bit integers.
- * An x that is not finite meets every weight of its row, zeros among them; other rows are not touched by it.  M == 0 is no work (pointers
+ * An x that is not finite meets every weight of its row, zeros among them (0 times infinity is NaN); other rows are not touched by it.  A sum that
+ * leaves 32 bits on its way is formed again in 64: infinities and the largest values give what the definition does, whatever M is, at the cost of
+ * up to 3 us for each such output.  M == 0 is no work (pointers
  * to x and y may be NULL then).  y must not overlap x.  workspace_dev: scratch of fscnn_linear_q4_workspace() bytes, 4-byte aligned, that belongs
  * to this call until it has run (and to a graph that captured it, as x and y do): the columns are then divided over work-groups, whose
  * sums lie there; NULL or less is right too, with sums in another order, and slower.  Allocates nothing, does not synchronise; results are

@@ -211,6 +211,7 @@ namespace fscnn {
 // zeros with a scale of zero.  A scale is the word of its value as a float, which 16-bit types leave at least 13 low bits of: the zero
 // point is in the low four.
 constexpr int kQ4Block = 128;
+__host__ __device__ inline int code_bit(int j) { return j < 4 ? 8 * j : 8 * (j - 4) + 4; }   // first bit of column j's code in its word
 inline long long q4_tiles(int K) { return ((long long)K + 15) / 16; }
 inline long long q4_blocks(int C) { return ((long long)C + kQ4Block - 1) / kQ4Block; }
 inline size_t q4_code_bytes(int K, int C) { return (size_t)q4_tiles(K) * q4_blocks(C) * 1024; }

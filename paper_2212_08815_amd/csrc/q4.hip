@@ -27,8 +27,6 @@ __device__ inline void word_at(const Shape &p, long long i, long long *row, int 
     *col = (int)(b % p.blocks) * kQ4Block + s * 32 + (lane >> 4) * 8;
 }
 
-__device__ inline int nibble_of(int j) { return j < 4 ? 8 * j : 8 * (j - 4) + 4; }   // first bit of column j's code
-
 __device__ inline uint32_t *scale_word(uint32_t *scales, const Shape &p, long long row, int g)
 {
     return scales + ((row >> 4) * p.groups + g) * 16 + (row & 15);
@@ -65,7 +63,7 @@ __global__ void __launch_bounds__(256) import_kernel(const Shape p, const unsign
         w = spread(lo) | spread(hi) << 4;
     } else if (live) {
         for (int j = 0; j < 8; ++j)
-            w |= (col + j < p.C ? codes[row * pitch + ((col + j) >> 1)] >> (4 * (j & 1)) & 15 : zero) << nibble_of(j);
+            w |= (col + j < p.C ? codes[row * pitch + ((col + j) >> 1)] >> (4 * (j & 1)) & 15 : zero) << code_bit(j);
     }
     out[i] = w;
     if (col % p.group == 0) {
@@ -118,7 +116,7 @@ __global__ void __launch_bounds__(256) compress_kernel(const Shape p, const void
         uint32_t code = zero;
         if (row < p.K && col + j < p.C && s > 0.0f)
             code = (uint32_t)fminf(fmaxf(rintf(load_float(w, row * ldw + col + j, type) / s) + z, 0.0f), 15.0f);
-        word |= code << nibble_of(j);
+        word |= code << code_bit(j);
     }
     out[i] = word;
 }
@@ -135,7 +133,7 @@ __global__ void __launch_bounds__(256) export_kernel(const Shape p, const uint32
     for (int e = 0; e < 2 && c + e < p.C; ++e) {
         const int at = (c + e) % kQ4Block, lane = (at / 8 % 4) * 16 + (int)(row & 15);
         const long long b = (row >> 4) * p.blocks + (c + e) / kQ4Block;
-        byte |= (in[(b * 64 + lane) * 4 + at / 32] >> nibble_of(at % 8) & 15) << (4 * e);
+        byte |= (in[(b * 64 + lane) * 4 + at / 32] >> code_bit(at % 8) & 15) << (4 * e);
     }
     codes[i] = (unsigned char)byte;
     if (c % p.group == 0) {

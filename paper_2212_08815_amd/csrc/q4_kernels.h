@@ -33,6 +33,7 @@ struct Q4Args {
     float *sums;                              // tile_kernel: [gridDim.y][M][16 tiles], where work-groups divide the blocks
     long long ldx, ldy;                       // ldx in bytes
     int K, C, M, blocks, tiles, steps, y_type, x_cols, act;   // steps: of 32 columns a group
+    int x_type;
     int mt, nt;                               // tile_kernel: tiles of the launch
 };
 
@@ -66,6 +67,52 @@ inline F32Choice f32_choice(long long tiles, int blocks, int M, int most)
 }
 
 namespace {
+
+__device__ inline bool finite(float v) { return fabsf(v) < __builtin_inff(); }
+
+// The sum of an output from the definition, entry by entry, in 64 bits, where no product or sum is too large: a row of x, its scales, and codes
+// and scales from the weight row's first on.  By a whole wave: four columns a lane, the lanes' sums added in a fixed order.  (No more than
+// four, and not inlined: the kernels' own registers are what counts.)
+__device__ __attribute__((noinline)) float sum_again(const char *row, int x_type, const float *x_scale, int x_cols, const uint32_t *codes, const uint32_t *scales, int C, int group)
+{
+    double sum = 0.0;
+#pragma unroll 1
+    for (int c = (threadIdx.x & 63) * 4; c < C; c += 256) {
+        const int g = c / group;
+        // (four codes of a parity: code_bit)
+        const uint32_t word = codes[(c >> 7) * 256LL + (c >> 3 & 3) * 64 + (c >> 5 & 3)] >> (c & 4), sz = scales[g * 16LL];
+        float x[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int at = c + j < C ? c + j : c;
+            x[j] = x_type == FSCNN_I8 ? (float)reinterpret_cast<const int8_t *>(row)[at] : load_float(row, at, x_type);
+        }
+        const double s = (double)__builtin_bit_cast(float, sz & ~15u), xs = x_scale ? (double)x_scale[x_cols > 1 ? g : 0] : 1.0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (c + j < C) sum += x[j] * xs * (((int)(word >> code_bit(j) & 15) - (int)(sz & 15)) * s);
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
+    return (float)sum;
+}
+
+// v of the wave's lanes, each the sum of output (m, k) if it is one (`real`): those that are not finite are made again.  A kernel's may be that
+// where the definition's is finite (codes times x, or a group's sum before it meets its scale, past the largest float), or NaN where it is
+// infinite (an infinite x in three parts, or less the zero point's share).  bf16, 4096 columns: 64 x 4096 outputs 16 us, 0.5 ms if those of one row are
+// made again; 4096 x 12288 415 us, 430 ms if all are.  Looking for them costs up to 2 % (0.1 us of the smallest calls).
+__device__ inline float mended(const Q4Args &a, bool real, int m, int k, float v)
+{
+    for (unsigned long long todo = __ballot(real && !finite(v)); __builtin_expect(todo != 0, 0); todo &= todo - 1) {
+        const int lane = __builtin_ctzll(todo), mm = __builtin_amdgcn_readlane(m, lane), kk = __builtin_amdgcn_readlane(k, lane);
+        const long long tile = kk >> 4;
+        const float s = sum_again(a.x + mm * a.ldx, a.x_type, a.x_scale ? a.x_scale + (long long)mm * a.x_cols : nullptr, a.x_cols,
+                                  reinterpret_cast<const uint32_t *>(a.codes) + (tile * a.blocks * 256 + (kk & 15) * 4),
+                                  a.scales + (tile * a.blocks * (64 >> (a.steps >> 1)) + (kk & 15)), a.C, a.steps * 32);
+        if ((int)(threadIdx.x & 63) == lane) v = s;
+    }
+    return v;
+}
 
 __device__ inline void store_output(const Q4Args &a, int m, int k, float v, float bias)
 {
@@ -105,17 +152,22 @@ template <int XT, class Acc> __device__ inline q4f4 add_group(const q4f4 &xs, ui
 // order of parts and waves
 template <int XT, int PARTS, int W> __device__ inline void store_sums(const Q4Args &a, const float *sums, int tile)
 {
-    for (int e = threadIdx.x; e < a.M * 16; e += W * 64) {
-        const int m = e >> 4, k = tile * 16 + (e & 15);
-        float f = 0.0f;
+    for (int e0 = 0; e0 < a.M * 16; e0 += W * 64) {
+        const int e = e0 + threadIdx.x, m = e >> 4, k = tile * 16 + (e & 15);
+        const bool real = m < a.M && k < a.K;
+        float f = 0.0f, bias = 0.0f;
+        if (real) {
+            if (a.bias) bias = a.bias[k];     // (on its way beside the reads of LDS)
 #pragma unroll
-        for (int p = 0; p < PARTS; ++p) {
-            const int row = m * PARTS + p, at = ((row >> 2) * 16 + (e & 15)) * 4 + (row & 3);
+            for (int p = 0; p < PARTS; ++p) {
+                const int row = m * PARTS + p, at = ((row >> 2) * 16 + (e & 15)) * 4 + (row & 3);
 #pragma unroll
-            for (int w = 0; w < W; ++w) f += sums[w * 256 + at];
+                for (int w = 0; w < W; ++w) f += sums[w * 256 + at];
+            }
+            if (XT == FSCNN_I8 && a.x_cols == 1) f *= a.x_scale[m];
         }
-        if (k >= a.K) continue;
-        store_output(a, m, k, XT == FSCNN_I8 && a.x_cols == 1 ? f * a.x_scale[m] : f, a.bias ? a.bias[k] : 0.0f);
+        f = mended(a, real, m, k, f);
+        if (real) store_output(a, m, k, f, bias);
     }
 }
 
@@ -333,10 +385,13 @@ __global__ void __launch_bounds__(WN * WK * 64, XT == FSCNN_F32 ? 1 : 2) tile_ke
     constexpr int kSums = (WK - 1) * kSet * MT * 4;  // in 16 bytes, at the end
     constexpr int kChunksOfSet = 2 * kBuf + kScales;
     static_assert(kPer * kSet == kRows * kCh, "a whole number of chunks a thread");
-    static_assert(!GS || kRows <= kSet, "a thread a row");
+    static_assert(kRows <= kSet * WK && (!GS || kRows <= kSet), "a thread a row");
+    static_assert(1024 * WN % (kSet * WK) == 0, "outputs in whole turns");
     constexpr int kPitch = 32 * WN + 8, kArea = 32 * kPitch;   // of outputs, in floats: rows 4 apart half of the banks apart
     constexpr int kNeed = kSums * 4 > 2 * kArea ? kSums : (2 * kArea + 3) / 4;
     __shared__ u4v lds[kChunksOfSet * WK > kNeed ? kChunksOfSet * WK : kNeed];
+    __shared__ int odd[MT];                   // rows of 32 whose sums are looked at again
+    if (threadIdx.x < MT) odd[threadIdx.x] = 0;   // (there is a barrier before they are read or set)
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wk = wave / WN, in_set = wave % WN, half = lane >> 5;
     // panels of 8 tiles of x: work-groups that run together share both operands
@@ -564,18 +619,24 @@ __global__ void __launch_bounds__(WN * WK * 64, XT == FSCNN_F32 ? 1 : 2) tile_ke
     float *const area = reinterpret_cast<float *>(lds);
     const int cols0 = n0 - in_set * 32;
     const auto put = [&](int u) {
+        float all[4] = {};
+        if (kInt && !GS && threadIdx.x < 32 && m0 + u * 32 + (int)threadIdx.x < a.M) all[0] = fabsf(a.x_scale[m0 + u * 32 + threadIdx.x]);
+        if (wk == 0)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) all[i & 3] += fabsf(total[u][i]);
+        if (!finite(all[0] + all[1] + (all[2] + all[3]))) odd[u] = 1;   // one of them is not, or (no harm) their sum alone
         if (wk == 0)
 #pragma unroll
             for (int i = 0; i < 16; ++i) area[(u & 1) * kArea + (8 * (i >> 2) + 4 * half + (i & 3)) * kPitch + in_set * 32 + (lane & 31)] = total[u][i];
     };
-    const auto store = [&](int u, auto type) {
+    const auto store = [&](int u, bool again, auto type) {
         using E = typename Elem<decltype(type)::value>::type;
         constexpr int kV = 16 / (int)sizeof(E), kRow = 32 * WN / kV;   // outputs of a thread; threads of a row
         for (int at = threadIdx.x; at < 32 * kRow; at += kSet * WK) {
             const int r = at / kRow, c = at % kRow * kV, m = m0 + u * 32 + r, k = cols0 + c;
             if (m >= a.M || k >= a.K) continue;
             const float *f = area + (u & 1) * kArea + r * kPitch + c;
-            const float xs = kInt && !GS ? a.x_scale[m] : 1.0f;
+            const float xs = kInt && !GS && !again ? a.x_scale[m] : 1.0f;
             E e[kV];
 #pragma unroll
             for (int j = 0; j < kV; ++j) {
@@ -591,14 +652,26 @@ __global__ void __launch_bounds__(WN * WK * 64, XT == FSCNN_F32 ? 1 : 2) tile_ke
                     if (k + j < a.K) y[j] = e[j];
         }
     };
+    const auto look = [&](int u) {            // (with the rows' scales; a whole number of turns for every wave)
+#pragma unroll 1
+        for (int at = threadIdx.x; at < 1024 * WN; at += kSet * WK) {
+            const int r = at / (32 * WN), m = m0 + u * 32 + r, k = cols0 + at % (32 * WN);
+            float *f = area + (u & 1) * kArea + r * kPitch + at % (32 * WN);
+            const bool real = m < a.M && k < a.K;
+            *f = mended(a, real, m, k, kInt && !GS && real ? *f * a.x_scale[m] : *f);
+        }
+        __syncthreads();
+    };
     __syncthreads();
 #pragma unroll
     for (int u = 0; u < MT; ++u) {            // (two areas: a barrier each)
         put(u);
         __syncthreads();
-        if (a.y_type == FSCNN_F32) store(u, std::integral_constant<int, FSCNN_F32>{});
-        else if (a.y_type == FSCNN_F16) store(u, std::integral_constant<int, FSCNN_F16>{});
-        else store(u, std::integral_constant<int, FSCNN_BF16>{});
+        const bool again = odd[u] != 0;       // (the same for all: written before the barrier only)
+        if (__builtin_expect(again, 0)) look(u);
+        if (a.y_type == FSCNN_F32) store(u, again, std::integral_constant<int, FSCNN_F32>{});
+        else if (a.y_type == FSCNN_F16) store(u, again, std::integral_constant<int, FSCNN_F16>{});
+        else store(u, again, std::integral_constant<int, FSCNN_BF16>{});
     }
 }
 

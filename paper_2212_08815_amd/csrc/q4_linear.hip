@@ -11,14 +11,18 @@ constexpr int kQ4LaunchRows = 1 << 18;
 template <int P> __global__ void __launch_bounds__(64) join_kernel(const Q4Args a)
 {
     const int k = (blockIdx.x * 64 + threadIdx.x) * 4;
-    if (k >= a.K) return;
     const long long pitch = a.tiles * 16LL;
     for (int m = blockIdx.y; m < a.M; m += gridDim.y) {
         q4f4 v[P];
+        v[0] = q4f4{};
+        if (k < a.K) {
 #pragma unroll
-        for (int p = 0; p < P; ++p) __builtin_memcpy(&v[p], a.sums + (((long long)p * a.M + m) * pitch + k), 16);
+            for (int p = 0; p < P; ++p) __builtin_memcpy(&v[p], a.sums + (((long long)p * a.M + m) * pitch + k), 16);
 #pragma unroll
-        for (int p = 1; p < P; ++p) v[0] += v[p];
+            for (int p = 1; p < P; ++p) v[0] += v[p];
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[0][i] = mended(a, k + i < a.K, m, k + i, v[0][i]);
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             if (k + i < a.K) store_output(a, m, k + i, v[0][i], a.bias ? a.bias[k + i] : 0.0f);
@@ -48,7 +52,7 @@ hipError_t launch_linear_q4(const fscnn_q4 *q, const void *x, int x_type, long l
         const Q4Args a = {reinterpret_cast<const u4v *>(q->codes), q->scales, static_cast<const char *>(x) + m * ldx * bytes,
                           x_scale ? x_scale + m * x_scale_cols : nullptr, bias, static_cast<char *>(y) + m * ldy * (y_type == FSCNN_F32 ? 4 : 2), sums,
                           ldx * bytes, ldy, q->K, q->C, (int)(M - m < kMost ? M - m : kMost), (int)q4_blocks(q->C), (int)q4_tiles(q->K),
-                          q->group / 32, y_type, x_scale_cols, act, 0, 0};
+                          q->group / 32, y_type, x_scale_cols, act, x_type, 0, 0};
         const int parts = sums ? q4_parts(q, x_type, M) : 1;
         hipError_t e;
         switch (x_type) {
