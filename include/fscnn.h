@@ -475,7 +475,8 @@ fscnn_status_t fscnn_q4_info(const fscnn_q4_t *q, int *K, int *C, int *group, in
 fscnn_status_t fscnn_q4_export(const fscnn_q4_t *q, unsigned char *codes_host, void *scales_host, unsigned char *zeros_host);
 fscnn_status_t fscnn_q4_destroy(fscnn_q4_t *q);
 
-/* y[m][k] = act(sum over c of w[k][c] * x[m][c] + bias_dev[k]),  act(a) = a > 0 ? a : negative_slope * a.
+/* y[m][k] = act(sum over c of w[k][c] * x[m][c] + bias_dev[k]),  act(a) = a > 0 ? a : negative_slope * a  (NaN where a is; 0 where a is
+ * -infinity and negative_slope 0).
  * x_dev: M rows of C elements of x_type, rows ldx >= C elements apart; y_dev: M rows of K elements of y_type (F32, F16, BF16), rows
  * ldy >= K elements apart, what lies between them is left as it is; both aligned to their type (16-byte aligned rows are read faster).
  * bias_dev: K floats or NULL.  negative_slope in [0, 1]: 1 no activation, 0 ReLU, between them LeakyReLU; else FSCNN_ERR_SHAPE.
@@ -484,8 +485,8 @@ fscnn_status_t fscnn_q4_destroy(fscnn_q4_t *q);
  * x_type I8: x[m][c] stands for x_dev[m][c] * x_scale, x_scale_dev M x x_scale_cols floats, one for the row (x_scale_cols 1) or one for
  * each group of the weights (ceil(C/group)); a group's sum is exact in 32-bit integers.
  * An x that is not finite meets every weight of its row, zeros among them (0 times infinity is NaN); other rows are not touched by it.  A sum that
- * leaves 32 bits on its way is formed again in 64: infinities and the largest values give what the definition does, whatever M is, at the cost of
- * up to 3 us for each such output.  M == 0 is no work (pointers
+ * leaves 32 bits on its way is formed again in 64: infinities and the largest values give what the definition does, whatever M is; a row of
+ * such outputs takes about half a millisecond.  M == 0 is no work (pointers
  * to x and y may be NULL then).  y must not overlap x.  workspace_dev: scratch of fscnn_linear_q4_workspace() bytes, 4-byte aligned, that belongs
  * to this call until it has run (and to a graph that captured it, as x and y do): the columns are then divided over work-groups, whose
  * sums lie there; NULL or less is right too, with sums in another order, and slower.  Allocates nothing, does not synchronise; results are

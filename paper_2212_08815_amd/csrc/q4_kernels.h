@@ -114,9 +114,12 @@ __device__ inline float mended(const Q4Args &a, bool real, int m, int k, float v
     return v;
 }
 
+// The activation, which leaves NaN as it is (act_apply's ReLU gives 0 for it, as the convolutions have it)
+__device__ inline float activated(float v, int act) { return act == 1 ? (v <= 0.0f ? 0.0f : v) : act_apply(v, act); }
+
 __device__ inline void store_output(const Q4Args &a, int m, int k, float v, float bias)
 {
-    store_float(a.y, m * a.ldy + k, a.y_type, act_apply(v + bias, a.act));
+    store_float(a.y, m * a.ldy + k, a.y_type, activated(v + bias, a.act));
 }
 
 // The scales of a group of rows m to m + 3 of x, where x has one for each group
@@ -642,7 +645,7 @@ __global__ void __launch_bounds__(WN * WK * 64, XT == FSCNN_F32 ? 1 : 2) tile_ke
             for (int j = 0; j < kV; ++j) {
                 float v = f[j];
                 if (kInt && !GS) v *= xs;
-                e[j] = (E)act_apply(v + (a.bias && k + j < a.K ? a.bias[k + j] : 0.0f), a.act);
+                e[j] = (E)activated(v + (a.bias && k + j < a.K ? a.bias[k + j] : 0.0f), a.act);
             }
             E *y = static_cast<E *>(a.y) + (m * a.ldy + k);
             if (k + kV <= a.K) __builtin_memcpy(y, e, 16);

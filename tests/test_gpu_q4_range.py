@@ -93,3 +93,27 @@ def test_eight_bits_with_scales_at_both_ends(F, m, rows):  # noqa: F811
     want = x64 @ w.t()
     want[0] = by_definition(x64[:1], w.cpu())
     assert same(F.linear_q4(h, x, x_scale=xs), want.float())
+
+
+@pytest.mark.parametrize("xt", FLOATS + [torch.int8], ids=["f32", "f16", "bf16", "i8"])
+@pytest.mark.parametrize("m", [1, 5, 16, 40, 300])
+def test_nan_through_the_activation(F, m, xt):  # noqa: F811
+    """What is NaN before a ReLU or LeakyReLU is NaN behind it, and nothing else is: of x, of its scales, of the bias."""
+    g = rng(m)
+    c, k = 300, 90
+    q, s, z = weights(g, k, c, 64, True, powers=True)
+    h = F.q4_import(packed(q), s, z, group=64, c=c)
+    x = ints(g, -3, 4, m, c).to(xt)
+    xs = torch.ones(m, device="cuda") if xt == torch.int8 else None
+    bias = ints(g, -5, 6, k).float()
+    bias[7], bias[8], bias[9] = float("nan"), INF, -INF
+    want = x.double() @ dense(q, s, z, 64)[0].t() + bias.double()
+    if xs is None:
+        x[-1, 3] = float("nan")
+    else:
+        xs[-1] = float("nan")
+    want[-1] = float("nan")
+    for act, y in ((dict(relu=True), want.clamp(min=0)), (dict(leaky=0.5), torch.where(want > 0, want, want * 0.5)), ({}, want)):
+        for yt in FLOATS:
+            got = F.linear_q4(h, x, bias=bias, x_scale=xs, out_dtype=yt, **act)
+            assert same(got, y.to(yt)) and not bool(torch.signbit(got[got == 0]).any())
