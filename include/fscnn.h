@@ -501,7 +501,8 @@ long long fscnn_linear_q4_workspace(const fscnn_q4_t *q, fscnn_dtype_t x_type, i
 
 /* Root-mean-square norm of M rows of D elements, with the residual's addition before it and an 8-bit output behind it:
  *   h = x (+ residual),   y = h / sqrt(mean over the row of h^2 + eps) * weight,
- * sums in fp32, h as it is before it is rounded.  x_dev, residual_dev (NULL: none) and residual_out_dev (receives h; NULL: not wanted; only
+ * sums in fp32, h as it is before it is rounded to x_type (an h past the largest float is infinite).  Squares that leave the range of fp32 do no
+ * harm: such a row is scaled by a power of two.  x_dev, residual_dev (NULL: none) and residual_out_dev (receives h; NULL: not wanted; only
  * with a residual) are of type x_type (F32, F16, BF16), weight_dev (NULL: ones) of weight_type, rows ldx, ldr, ldo, ldy >= D elements apart.
  * y_type F32, F16, BF16: scale_dev NULL, group 0.  y_type I8: y_dev receives rint(y / scale) in -127..127 with
  * scale = max|y| / 127 over the row (group 0, scale_dev M floats) or over each group of 32, 64 or 128 elements (scale_dev

@@ -124,16 +124,40 @@ template <int T, int N, int TH, bool Q8> __global__ void __launch_bounds__(TH < 
         }
         if (a.ro) store_vec<T, V>(a.ro + m * a.ldo, (i * TH + t) * V, a.D, h[i]);
     }
+    // the row's sum from its threads'
+    const auto of_row = [&](float v) {
 #pragma unroll
-    for (int d = 1; d < 64 && d < TH; d *= 2) sum += __shfl_xor(sum, d);
-    if constexpr (kWaves > 1) {
-        if (lane == 0) sums[wave] = sum;
-        __syncthreads();
+        for (int d = 1; d < 64 && d < TH; d *= 2) v += __shfl_xor(v, d);
+        if constexpr (kWaves > 1) {
+            if (lane == 0) sums[wave] = v;
+            __syncthreads();
+            v = 0.0f;
+#pragma unroll
+            for (int i = 0; i < kWaves; ++i) v += sums[i];
+        }
+        return v;
+    };
+    sum = of_row(sum);
+    float f = 1.0f / sqrtf(sum / (float)a.D + a.eps);
+    // Squares past the largest float, or so small that they lost digits: h by a power of two closer to 1, and its squares again.  (The same for all
+    // threads of a row.  2^-80 takes the largest rows' mean square to 2^96, 2^96 that of rows below 2^-90 to at most 2^102; what
+    // is lost at the other end does not show beside it.)
+    if (__builtin_expect(!(sum < __builtin_inff()) || sum / (float)a.D + a.eps < 0x1p-90f, 0)) {
+        const bool large = !(sum < 1.0f);
+        const float by = large ? 0x1p-80f : 0x1p96f;
         sum = 0.0f;
 #pragma unroll
-        for (int i = 0; i < kWaves; ++i) sum += sums[i];
+        for (int i = 0; i < N; ++i)
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const float v = h[i][j] * by;
+                sum = __builtin_fmaf(v, v, sum);
+                h[i][j] = large ? h[i][j] * 0x1p-40f : v;   // (the other half with f: neither is then below the normal numbers)
+            }
+        if constexpr (kWaves > 1) __syncthreads();
+        sum = of_row(sum);
+        f = 1.0f / sqrtf(sum / (float)a.D + a.eps * by * by) * (large ? 0x1p-40f : 1.0f);
     }
-    const float f = 1.0f / sqrtf(sum / (float)a.D + a.eps);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         const int c = (i * TH + t) * V;
