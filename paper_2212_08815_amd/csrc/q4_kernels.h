@@ -688,24 +688,30 @@ template <int XT, int W> hipError_t launch_rows(const Q4Args &a, hipStream_t st)
     return hipGetLastError();
 }
 
+constexpr int kMostStaged = 144 << 10;       // bytes of LDS
+
+// (named by its template: kernels of one signature would share the static of a function that is handed one)
+template <int XT, int W, int STEPS> hipError_t launch_staged_steps(const Q4Args &a, int cols, int bytes, hipStream_t st)
+{
+    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void *>(&staged_kernel<XT, W, STEPS>),
+                                                       hipFuncAttributeMaxDynamicSharedMemorySize, kMostStaged);
+    if (attr != hipSuccess) return attr;
+    hipLaunchKernelGGL((staged_kernel<XT, W, STEPS>), dim3(a.tiles), dim3(W * 64), bytes, st, a, cols);
+    return hipGetLastError();
+}
+
 template <int XT, int W> hipError_t launch_staged(const Q4Args &a, hipStream_t st)
 {
-    constexpr int kBytes = XT == FSCNN_I8 ? 1 : 2, kMost = 144 << 10, kTurn = W * kQ4Block;
+    constexpr int kBytes = XT == FSCNN_I8 ? 1 : 2, kMost = kMostStaged, kTurn = W * kQ4Block;
     const int rows = a.M * XOp<XT>::kParts;
     if (rows > 16 || a.tiles * (W * 64LL) > 0xffffffffLL) return hipErrorInvalidValue;
     // as many columns in LDS as leave room for a second work-group where there is one for a CU
     const int room = a.tiles > 256 ? kMost / 2 : kMost, fit = (room / rows - 16) / kBytes / kTurn * kTurn, all = a.blocks * kQ4Block;
-    const int cols = all < fit ? all : fit, bytes = rows * (cols * kBytes + 16), sums = W * 1024;
+    const int cols = all < fit ? all : fit, staged = rows * (cols * kBytes + 16), sums = W * 1024, bytes = staged > sums ? staged : sums;
     static_assert(16 * (kTurn * kBytes + 16) <= kMost / 2, "a turn of 16 rows fits");
-    auto launch = [&](auto kernel) {
-        static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, kMost);
-        if (attr != hipSuccess) return attr;
-        hipLaunchKernelGGL(kernel, dim3(a.tiles), dim3(W * 64), bytes > sums ? bytes : sums, st, a, cols);
-        return hipGetLastError();
-    };
-    if (a.steps == 1) return launch(&staged_kernel<XT, W, 1>);
-    if (a.steps == 2) return launch(&staged_kernel<XT, W, 2>);
-    return launch(&staged_kernel<XT, W, 4>);
+    if (a.steps == 1) return launch_staged_steps<XT, W, 1>(a, cols, bytes, st);
+    if (a.steps == 2) return launch_staged_steps<XT, W, 2>(a, cols, bytes, st);
+    return launch_staged_steps<XT, W, 4>(a, cols, bytes, st);
 }
 
 template <int XT, int MT, int WN, int WK, bool DMA, bool GS> hipError_t launch_tiles(Q4Args a, int parts, hipStream_t st)
