@@ -1707,8 +1707,10 @@ fscnn_status_t fscnn_q4_import(const unsigned char *codes_dev, const void *scale
     if (s != FSCNN_OK) return s;
     int *flag = reinterpret_cast<int *>(reinterpret_cast<char *>(q->scales) + q4_scale_bytes(K, C, group)), bad = 0;
     hipError_t e = launch_q4_import(q, codes_dev, scales_dev, zeros_dev, flag, (hipStream_t)stream);
-    if (e == hipSuccess) e = hipStreamSynchronize((hipStream_t)stream);
-    if (e == hipSuccess && zeros_dev) e = hipMemcpy(&bad, flag, sizeof(int), hipMemcpyDeviceToHost);
+    // (on the call's stream: a copy on the default one waits for streams that have nothing to do with it)
+    if (e == hipSuccess && zeros_dev) e = hipMemcpyAsync(&bad, flag, sizeof(int), hipMemcpyDeviceToHost, (hipStream_t)stream);
+    const hipError_t waited = hipStreamSynchronize((hipStream_t)stream);   // (whatever came before: `bad` may be written until then)
+    if (e == hipSuccess) e = waited;
     if (e != hipSuccess || bad) {
         (void)hipGetLastError();
         q4_delete(q);
