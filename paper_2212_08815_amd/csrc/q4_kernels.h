@@ -20,6 +20,7 @@
 
 #include "internal.h"
 #include "lds_dma.h"
+#include "q4_choice.h"
 #include "q4_tile.h"
 
 namespace fscnn {
@@ -36,35 +37,6 @@ struct Q4Args {
     int x_type;
     int mt, nt;                               // tile_kernel: tiles of the launch
 };
-
-// Columns divided over `parts` work-groups cost a second launch, and the sums' way to memory and back (us)
-inline double sums_us(double M, double tiles, int parts) { return parts > 1 ? 2.5 + parts * 1.28e-4 * M * tiles / 3 : 0; }
-
-// How 32-bit floats are served: kernel, and work-groups that divide the columns, at most `most` of them
-struct F32Choice {
-    enum Kernel { kStaged, kRows, kTile32, kTile64 } kernel;
-    int parts;
-};
-inline F32Choice f32_choice(long long tiles, int blocks, int M, int most)
-{
-    // (25088 -> 4096, one row: 14.1 us staged, 30 with a wave's own parts)
-    if (M * XOp<FSCNN_F32>::kParts <= 16) return {F32Choice::kStaged, 1};
-    // times of launches as TileCost has them; divided columns cost a launch and the sums' way to memory and back
-    const double wide = (double)((tiles + 15) / 16);   // work-groups of a part of 32 or 64 rows
-    F32Choice best = {F32Choice::kTile32, 1};
-    double us = 1e30;
-    for (int rows = 32; rows <= 64; rows *= 2)
-        for (int p = 1; p <= most && p <= 16 && blocks / p >= 4; p *= 2) {
-            const double n = __builtin_ceil(wide * ((M + rows - 1) / rows) * p / 256);
-            const double t = 4 + n * ((blocks + p - 1) / p) * (rows == 32 ? 1.45 : 2.65) + sums_us(M, (double)tiles, p);
-            if (t < us) {
-                us = t;
-                best = {rows == 32 ? F32Choice::kTile32 : F32Choice::kTile64, p};
-            }
-        }
-    if (M <= 16 && 4 + __builtin_ceil(tiles / 256.0) * (blocks / 32.0) * (4 + 0.3 * M) < us) return {F32Choice::kRows, 1};
-    return best;
-}
 
 namespace {
 
@@ -731,18 +703,6 @@ template <int XT, int MT, int WN, int WK, bool DMA, bool GS> hipError_t launch_t
 // x may go to LDS without registers: 16-byte loads, offsets of a tile's rows below 2^31
 inline bool dma_serves(const Q4Args &a, int rows) { return !(((uintptr_t)a.x | (uintptr_t)a.ldx) & 15) && a.ldx * rows < 0x7fff0000LL; }
 
-// Time of a launch in us: 4 and, for every turn (a block a set of waves), `one` while a CU has a work-group, `many` times the work-groups of a CU beyond
-// that; `parts` work-groups divide the columns
-struct TileCost {
-    int rows, cols, sets;
-    float one, many;
-    double us(double M, double K, int blocks, int parts) const
-    {
-        const double groups = __builtin_ceil(M / rows) * __builtin_ceil(K / cols) * parts, n = __builtin_ceil(groups / 256);
-        return 4 + ((blocks + parts - 1) / parts + sets - 1) / sets * (n > 1 && many * n > one ? many * n : one);
-    }
-};
-
 template <int XT, int MT, int WN, int WK, bool DMA> hipError_t launch_tiles(const Q4Args &a, int parts, hipStream_t st)
 {
     if constexpr (XT == FSCNN_I8)
@@ -750,61 +710,17 @@ template <int XT, int MT, int WN, int WK, bool DMA> hipError_t launch_tiles(cons
     return launch_tiles<XT, MT, WN, WK, DMA, false>(a, parts, st);
 }
 
-// x in 16 or 8 bits.  The fastest of seven shapes of tile_kernel, in 8 bits five, by what launches of them take (fitted to 1 to 4096 rows, 1024 to
-// 16384 columns, 1024 to 12288 weight rows, within 15 %; in 16 bits the choice is 0.4 % behind the fastest in the mean, in 8 bits 2.4): many sets
-// where few work-groups are there, whose sums through LDS cost more than they bring where they are many (bf16, 4096 -> 4096: 64 rows of x 9.3 us
-// with 32 x 32 in 8 sets, 28 with 64 x 128 in one; 1024 rows 117 and 45), and the shape whose work-groups leave the fewest CUs idle (200 rows
-// 17.4 us with 64 x 64 in 4 sets, 19.4 with the best of the others; 700 rows 33.3 with 96 x 128 in 2 sets and 39.2).  Rows of x that
-// are not 16 bytes aligned come by way of registers and have four shapes (fp16, 4097 -> 4096: 64 rows 15.4 us with 32 x 32 in 8 sets, 36 with
-// 64 x 128 in one; 2048 rows 407 and 94).  Up to 16 rows also staged_kernel and, for one or two rows, whose operand is
-// not worth a barrier, rows_kernel (bf16, 4096 -> 4096: one row 3.7 us, 4.1 staged; 8 rows 5.5 and 4.9).  Sixteen waves where a wave of
-// eight had eight blocks or more (one row of 16384: 8.3 us, 10.3 with eight; of 4096: 3.9 and 3.7).
-struct NarrowChoice {
-    int shape;
-    double us;
-};
-template <int XT> NarrowChoice narrow_choice(double M, double K, int blocks, int parts, bool dma)
-{
-    constexpr bool kInt = XT == FSCNN_I8;
-    constexpr TileCost kTiles[7] = {{32, 32, 8, kInt ? 0.68f : 1.3f, kInt ? 0.8f : 1.55f}, {32, 64, 4, kInt ? 0.6f : 1.0f, kInt ? 0.6f : 0.93f},
-                                    {64, 128, 2, kInt ? 0.8f : 1.3f, kInt ? 0.79f : 1.2f}, {64, 128, 1, kInt ? 0.52f : 0.8f, kInt ? 0.41f : 0.62f},
-                                    {128, 128, 1, kInt ? 0.9f : 1.25f, kInt ? 0.72f : 1.08f}, {64, 64, 4, 1.6f, 1.72f}, {96, 128, 2, 1.65f, 1.78f}};
-    constexpr TileCost kLoose[4] = {{32, 32, 8, kInt ? 1.5f : 2.1f, kInt ? 1.3f : 2.5f}, {32, 64, 4, kInt ? 1.05f : 1.28f, kInt ? 0.82f : 1.04f},
-                                    {64, 128, 2, kInt ? 1.26f : 1.54f, kInt ? 1.42f : 1.6f}, {64, 128, 1, kInt ? 0.8f : 1.0f, kInt ? 0.56f : 0.69f}};
-    NarrowChoice best = {0, 1e30};
-    for (int i = 0; i < (!dma ? 4 : kInt ? 5 : 7); ++i)
-        if (const double t = (dma ? kTiles[i] : kLoose[i]).us(M, K, blocks, parts); t < best.us) best = {i, t};
-    return best;
-}
-
-// Work-groups that divide the columns of more than 16 rows of x, at most `most`: where few weight rows leave CUs without one (64 rows, 20000 -> 300:
-// bf16 29.6 us, 11.2 in 16 parts; 200 rows, 25088 -> 512 35.4 and 22.6 in 8; int8 19.6 and 12.3 in 8)
-template <int XT> int narrow_parts(double M, long long tiles, int K, int blocks, int most)
-{
-    int best = 1;
-    double us = narrow_choice<XT>(M, K, blocks, 1, true).us;
-    for (int p = 2; p <= most && p <= 16 && blocks / p >= 4; p *= 2)
-        if (const double t = narrow_choice<XT>(M, K, blocks, p, true).us + sums_us(M, (double)tiles, p); t < us) {
-            us = t;
-            best = p;
-        }
-    return best;
-}
-
 template <int XT> hipError_t launch_narrow(const Q4Args &a, int parts, hipStream_t st)
 {
     constexpr bool kInt = XT == FSCNN_I8;
     const bool dma = dma_serves(a, 128);
-    const NarrowChoice best = narrow_choice<XT>(a.M, a.K, a.blocks, parts, dma);
-    if (a.M <= 16 && parts == 1) {
-        const int n = (a.tiles + 255) / 256;
-        const bool deep = a.blocks >= 64 && n == 1;
-        if (a.M <= 4 || 2.9f + n * (a.blocks / 32.0f) * (0.95f + 0.13f * a.M) <= best.us) {
-            if (a.M > 2) return deep ? launch_staged<XT, 16>(a, st) : launch_staged<XT, 8>(a, st);
-            return deep ? launch_rows<XT, 16>(a, st) : launch_rows<XT, 8>(a, st);
-        }
+    const Q4Choice c = narrow_choice(kInt, a.M, a.K, a.blocks, parts, dma);
+    switch (c.kernel) {
+        case Q4Choice::kRows: return c.waves == 16 ? launch_rows<XT, 16>(a, st) : launch_rows<XT, 8>(a, st);
+        case Q4Choice::kStaged: return c.waves == 16 ? launch_staged<XT, 16>(a, st) : launch_staged<XT, 8>(a, st);
+        default: break;
     }
-    switch (best.shape) {
+    switch (c.shape) {
         case 0: return dma ? launch_tiles<XT, 1, 1, 8, true>(a, parts, st) : launch_tiles<XT, 1, 1, 8, false>(a, parts, st);
         case 1: return dma ? launch_tiles<XT, 1, 2, 4, true>(a, parts, st) : launch_tiles<XT, 1, 2, 4, false>(a, parts, st);
         case 2: return dma ? launch_tiles<XT, 2, 4, 2, true>(a, parts, st) : launch_tiles<XT, 2, 4, 2, false>(a, parts, st);
@@ -817,7 +733,7 @@ template <int XT> hipError_t launch_narrow(const Q4Args &a, int parts, hipStream
 
 }  // namespace
 
-// parts: work-groups that divide the columns (32-bit floats: q4_parts(); else 1)
+// parts: work-groups that divide the columns: q4_parts(), or 1 where a call has no room for their sums
 template <int XT> hipError_t launch_q4_type(const Q4Args &a, int parts, hipStream_t st);
 template <> hipError_t launch_q4_type<FSCNN_F32>(const Q4Args &a, int parts, hipStream_t st);
 template <> hipError_t launch_q4_type<FSCNN_F16>(const Q4Args &a, int parts, hipStream_t st);

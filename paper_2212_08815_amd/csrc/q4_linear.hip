@@ -5,8 +5,6 @@ namespace fscnn {
 
 namespace {
 
-constexpr int kQ4LaunchRows = 1 << 18;
-
 // What the P work-groups that divide the columns have left, added in their order; four outputs a thread, all loads on their way together
 template <int P> __global__ void __launch_bounds__(64) join_kernel(const Q4Args a)
 {
@@ -31,17 +29,7 @@ template <int P> __global__ void __launch_bounds__(64) join_kernel(const Q4Args 
 
 }  // namespace
 
-int q4_parts(const fscnn_q4 *q, int x_type, int M)
-{
-    // (a launch's rows of x: the sums' room is for one launch, and bounded)
-    constexpr double kMostBytes = 64 << 20;
-    if (M <= (x_type == FSCNN_F32 ? 0 : 16) || M > kQ4LaunchRows) return 1;
-    const long long tiles = q4_tiles(q->K);
-    const int blocks = (int)q4_blocks(q->C), most = (int)(kMostBytes / (64.0 * tiles * M));
-    if (x_type == FSCNN_F32) return f32_choice(tiles, blocks, M, most > 1 ? most : 1).parts;
-    if (x_type == FSCNN_I8) return narrow_parts<FSCNN_I8>(M, tiles, q->K, blocks, most);
-    return narrow_parts<FSCNN_BF16>(M, tiles, q->K, blocks, most);
-}
+int q4_parts(const fscnn_q4 *q, int x_type, int M) { return q4_parts(x_type, M, q->K, q->C); }
 
 hipError_t launch_linear_q4(const fscnn_q4 *q, const void *x, int x_type, long long ldx, const float *x_scale, int x_scale_cols, int M,
                             const float *bias, int act, void *y, int y_type, long long ldy, float *sums, hipStream_t st)
