@@ -26,8 +26,9 @@ inline Q4Choice f32_choice(long long tiles, int blocks, int M, int most)
     // times of launches as TileCost has them; divided columns cost a launch and the sums' way to memory and back
     const double wide = (double)((tiles + 15) / 16);   // work-groups of a part of 32 or 64 rows
     Q4Choice best = {Q4Choice::kTiles, 0, 32, 1, 1e30};
-    for (int rows = 32; rows <= 64; rows *= 2)
-        for (int p = 1; p <= most && p <= 16 && blocks / p >= 4; p *= 2) {
+    // (up to 384 columns stores are what counts: 4096 rows to 16384 of 384 take 198 us in tiles of 32 rows, 254 in tiles of 64)
+    for (int rows = 32; rows <= (blocks < 4 ? 32 : 64); rows *= 2)
+        for (int p = 1; p == 1 || (p <= most && p <= 16 && blocks / p >= 4); p *= 2) {
             const double n = __builtin_ceil(wide * ((M + rows - 1) / rows) * p / 256);
             const double t = 4 + n * ((blocks + p - 1) / p) * (rows == 32 ? 1.45 : 2.65) + sums_us(M, (double)tiles, p);
             if (t < best.us) best = {Q4Choice::kTiles, 0, rows, p, t};

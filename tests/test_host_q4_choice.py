@@ -1,0 +1,47 @@
+"""Which kernel serves a product with 4-bit weights (csrc/q4_choice.h), compiled and asked on the CPU."""
+import os
+import subprocess
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+PROGRAM = r"""
+#include "q4_choice.h"
+#include <cstdio>
+using namespace fscnn;
+int main()                                     // x_type M K C aligned room  ->  kernel waves shape parts us
+{
+    int t, M, K, C, aligned, room;
+    while (std::scanf("%d %d %d %d %d %d", &t, &M, &K, &C, &aligned, &room) == 6) {
+        const int parts = room ? q4_parts(t, M, K, C) : 1, blocks = (C + 127) / 128, rows = M < kQ4LaunchRows ? M : kQ4LaunchRows;
+        const Q4Choice c = t == FSCNN_F32 ? f32_choice((K + 15LL) / 16, blocks, rows, parts) : narrow_choice(t == FSCNN_I8, rows, K, blocks, parts, aligned);
+        std::printf("%d %d %d %d %g\n", c.kernel, c.waves, c.shape, parts, c.us);
+    }
+}
+"""
+F32, F16, BF16, I8 = range(4)
+ROWS, STAGED, TILES = range(3)
+
+
+@pytest.fixture(scope="module")
+def ask(tmp_path_factory):
+    d = tmp_path_factory.mktemp("choice")
+    (d / "choice.cpp").write_text(PROGRAM)
+    subprocess.run(["g++", "-std=c++17", "-O1", "-I", os.path.join(ROOT, "include"), "-I", os.path.join(ROOT, "paper_2212_08815_amd", "csrc"),
+                    str(d / "choice.cpp"), "-o", str(d / "choice")], check=True)
+
+    def f(cases):
+        r = subprocess.run([str(d / "choice")], input="\n".join(" ".join(map(str, map(int, c))) for c in cases), capture_output=True, text=True, check=True)
+        return [(int(a[0]), int(a[1]), int(a[2]), int(a[3]), float(a[4])) for a in (line.split() for line in r.stdout.splitlines())]
+    return f
+
+
+def test_few_columns_of_fp32(ask):
+    """Fewer than four blocks of columns: the cheaper of a wave's own rows and tiles, as with more (16 rows to 60000 of 384: 20.2 us the former, 10.5
+    tiles); tiles of 32 rows for more rows."""
+    sizes = [(6, 60000, 384), (16, 60000, 384), (16, 30000, 256), (10, 60000, 128), (6, 4096, 300), (16, 4096, 384), (12, 12288, 384), (17, 60000, 384), (4096, 16384, 384),
+             (900, 8200, 300), (40, 1000, 1)]
+    want = [TILES] * 4 + [ROWS] * 3 + [TILES] * 4
+    for room in (0, 1):
+        got = ask([(F32, m, k, c, 1, room) for m, k, c in sizes])
+        assert [c[0] for c in got] == want and all(c[2] == 32 for c in got if c[0] == TILES) and all(c[3] == 1 and c[4] < 1e4 for c in got)
