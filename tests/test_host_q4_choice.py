@@ -1,5 +1,7 @@
 """Which kernel serves a product with 4-bit weights (csrc/q4_choice.h), compiled and asked on the CPU."""
+import math
 import os
+import random
 import subprocess
 
 import pytest
@@ -45,3 +47,21 @@ def test_few_columns_of_fp32(ask):
     for room in (0, 1):
         got = ask([(F32, m, k, c, 1, room) for m, k, c in sizes])
         assert [c[0] for c in got] == want and all(c[2] == 32 for c in got if c[0] == TILES) and all(c[3] == 1 and c[4] < 1e4 for c in got)
+
+
+def served(ask, sizes):
+    """What serves calls of these sizes, in every type, with their rows 16 bytes aligned and not, with scratch and without; and into how many parts columns
+    are divided."""
+    calls = [(t, m, k, c, al, room) for m, c, k in sizes for t in (F32, F16, I8) for al in ((0, 1) if t != F32 else (1,)) for room in (0, 1)]
+    out = set()
+    for (t, m, k, c, al, room), (kernel, waves, shape, parts, _) in zip(calls, ask(calls)):
+        out |= {(t, kernel, waves, shape, parts > 1, al), (t, parts)}
+    return out
+
+
+def test_the_gpu_tests_reach_every_kernel(ask):
+    """What the choice gives for 50 thousand sizes of all magnitudes is run by tests/test_gpu_q4_groups.py, there with every group size and way of scaling."""
+    from test_gpu_q4_groups import CASES
+    r = random.Random(3)
+    any_size = lambda hi: int(round(math.exp(r.uniform(0, math.log(hi)))))
+    assert served(ask, [(any_size(20000), any_size(1 << 20), any_size(60000)) for _ in range(50000)]) <= served(ask, CASES)
