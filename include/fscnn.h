@@ -457,7 +457,7 @@ typedef struct fscnn_q4 fscnn_q4_t;
  * lo = min(0, w), hi = max(0, w).  The scale is rounded to fp16 for fp16 weights and to bf16 otherwise, and
  * code = min(max(rint(w / scale) + zero, 0), 15) with the rounded scale; a group of zeros has scale 0, one with an infinite weight or a NaN
  * scale NaN.  Runs on `stream` and waits until the handle is written: then w_dev may go and any stream use the handle.  A capturing
- * stream is refused (FSCNN_ERR_UNSUPPORTED).  C up to 2^20. */
+ * stream is refused (FSCNN_ERR_UNSUPPORTED).  C up to 2^20, K up to 2^27 - 16. */
 fscnn_status_t fscnn_q4_compress(const void *w_dev, fscnn_dtype_t w_type, int K, int C, long long ldw, int group, int zeros,
                                  void *stream, fscnn_q4_t **out);
 

@@ -10,6 +10,7 @@
 
 #include "host_word.h"
 #include "internal.h"
+#include "q4_choice.h"
 
 using namespace fscnn;
 
@@ -1643,7 +1644,7 @@ static fscnn_status_t q4_new(int K, int C, int group, int zeros, int type, hipSt
 {
     if (K <= 0 || C <= 0) return FSCNN_ERR_SHAPE;
     if (group != 32 && group != 64 && group != 128) return FSCNN_ERR_UNSUPPORTED;
-    if (C > 1 << 20) return FSCNN_ERR_UNSUPPORTED;
+    if (C > 1 << 20 || K > kQ4MostRows) return FSCNN_ERR_UNSUPPORTED;
     int dev;
     fscnn_status_t s = have_device(&dev);
     if (s != FSCNN_OK) return s;

@@ -4,7 +4,15 @@
 
 namespace fscnn {
 
-constexpr int kQ4LaunchRows = 1 << 18;       // rows of x a launch
+constexpr int kQ4MostRows = (1 << 27) - 16;  // weight rows: 512 threads for 16 of them, fewer than 2^32 in a launch
+constexpr int kQ4LaunchRows = 1 << 18;       // rows of x a launch, at most
+// The rows of x a launch: its tiles, at worst 512 threads for 32 x 32 outputs, are fewer than 2^32 threads
+inline int q4_launch_rows(int K)
+{
+    int rows = kQ4LaunchRows;
+    while (rows > 32 && rows / 32 * ((K + 31LL) / 32) * 512 > 0xffffffffLL) rows /= 2;
+    return rows;
+}
 
 struct Q4Choice {
     enum Kernel { kRows, kStaged, kTiles } kernel;

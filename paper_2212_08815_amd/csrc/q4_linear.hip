@@ -35,11 +35,11 @@ hipError_t launch_linear_q4(const fscnn_q4 *q, const void *x, int x_type, long l
                             const float *bias, int act, void *y, int y_type, long long ldy, float *sums, hipStream_t st)
 {
     const int bytes = x_type == FSCNN_F32 ? 4 : x_type == FSCNN_I8 ? 1 : 2;
-    constexpr long long kMost = kQ4LaunchRows;   // rows of x in launches that a grid holds
-    for (long long m = 0; m < M; m += kMost) {
+    const long long most = q4_launch_rows(q->K);   // rows of x in launches that a grid holds
+    for (long long m = 0; m < M; m += most) {
         const Q4Args a = {reinterpret_cast<const u4v *>(q->codes), q->scales, static_cast<const char *>(x) + m * ldx * bytes,
                           x_scale ? x_scale + m * x_scale_cols : nullptr, bias, static_cast<char *>(y) + m * ldy * (y_type == FSCNN_F32 ? 4 : 2), sums,
-                          ldx * bytes, ldy, q->K, q->C, (int)(M - m < kMost ? M - m : kMost), (int)q4_blocks(q->C), (int)q4_tiles(q->K),
+                          ldx * bytes, ldy, q->K, q->C, (int)(M - m < most ? M - m : most), (int)q4_blocks(q->C), (int)q4_tiles(q->K),
                           q->group / 32, y_type, x_scale_cols, act, x_type, 0, 0};
         const int parts = sums ? q4_parts(q, x_type, M) : 1;
         hipError_t e;

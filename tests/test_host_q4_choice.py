@@ -65,3 +65,43 @@ def test_the_gpu_tests_reach_every_kernel(ask):
     r = random.Random(3)
     any_size = lambda hi: int(round(math.exp(r.uniform(0, math.log(hi)))))
     assert served(ask, [(any_size(20000), any_size(1 << 20), any_size(60000)) for _ in range(50000)]) <= served(ask, CASES)
+
+
+LAUNCHES = r"""
+#include "q4_choice.h"
+#include <cstdio>
+using namespace fscnn;
+int main()                                     // K -> rows of x a launch
+{
+    int K;
+    std::printf("%d\n", kQ4MostRows);
+    while (std::scanf("%d", &K) == 1) std::printf("%d\n", q4_launch_rows(K));
+}
+"""
+
+
+def test_a_launch_holds_its_threads(ask, tmp_path):
+    """Fewer than 2^32 threads for any number of rows of x and of weights: tiles by the choice's shapes, 16 weight rows a work-group where x has few rows."""
+    (tmp_path / "launch.cpp").write_text(LAUNCHES)
+    subprocess.run(["g++", "-std=c++17", "-I", os.path.join(ROOT, "include"), "-I", os.path.join(ROOT, "paper_2212_08815_amd", "csrc"), str(tmp_path / "launch.cpp"),
+                    "-o", str(tmp_path / "launch")], check=True)
+    r = random.Random(5)
+    most = 2 ** 27 - 16
+    ks = [1, 32768, 32769, 262145, 1 << 20, most - 1, most] + [int(2 ** r.uniform(0, 27)) for _ in range(300)]
+    ks = [min(k, most) for k in ks]
+    out = subprocess.run([str(tmp_path / "launch")], input=" ".join(map(str, ks)), capture_output=True, text=True, check=True).stdout.split()
+    assert int(out[0]) == most
+    tiles = {F32: {32: (32, 256, 512), 64: (64, 256, 512)},
+             F16: dict(enumerate([(32, 32, 512), (32, 64, 512), (64, 128, 512), (64, 128, 256), (128, 128, 256), (64, 64, 512), (96, 128, 512)]))}
+    tiles[I8] = tiles[F16]
+    up = lambda a, b: -(-a // b)
+    for k, rows in zip(ks, map(int, out[1:])):
+        assert 32 <= rows <= 1 << 18 and (k > 30000 or rows == 1 << 18)
+        calls = [(t, m, k, c, al, 1) for t in tiles for al in (0, 1) for m in (1, 5, 16, rows // 2 + 1, rows) for c in (1, 128, 600, 5000)]
+        for (t, m, *_), (kernel, waves, shape, parts, _) in zip(calls, ask(calls)):
+            if kernel == TILES:
+                a, b, threads = tiles[t][shape]
+                n = up(m, a) * up(k, b) * threads      # (parts are the grid's second dimension)
+            else:
+                n = up(k, 16) * waves * 64
+            assert n < 2 ** 32
