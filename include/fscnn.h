@@ -481,7 +481,8 @@ fscnn_status_t fscnn_q4_destroy(fscnn_q4_t *q);
  * ldy >= K elements apart, what lies between them is left as it is; both aligned to their type (16-byte aligned rows are read faster).
  * bias_dev: K floats or NULL.  negative_slope in [0, 1]: 1 no activation, 0 ReLU, between them LeakyReLU; else FSCNN_ERR_SHAPE.
  * x_type F32, F16, BF16: x_scale_dev NULL; products are formed with the codes, or with code - zero (both exact), sums are held in fp32 and every group's
- * is multiplied by its scale in fp32; y is rounded once.  (F32: x enters as three bfloat16 parts, their sum within 2^-24 of it.)
+ * is multiplied by its scale in fp32; y is rounded once.  (F32: x enters as three bfloat16 parts,
+ * their sum within 2^-24 of it, or within 2^-133 where that is more.)
  * x_type I8: x[m][c] stands for x_dev[m][c] * x_scale, x_scale_dev M x x_scale_cols floats, one for the row (x_scale_cols 1) or one for
  * each group of the weights (ceil(C/group)); a group's sum is exact in 32-bit integers.
  * An x that is not finite meets every weight of its row, zeros among them (0 times infinity is NaN); other rows are not touched by it.  A sum that

@@ -8,7 +8,8 @@
 // (codes.  weights, with the zero point subtracted, take 2.4 instructions a code and are for tiles of many rows, and for the products of three
 // parts: where these meet in one sum, it and the one of x lose a digit, 2.4e-6 of the result instead of 1.3e-7 over 4096 columns that
 // are not negative.  In sums of their own the parts' errors are alike and their difference has few of them: 2.5e-7.)
-// Floats enter as three bfloat16 parts (8 bits of the significand each, by truncation: their sum is the float), integers as they are.
+// Floats enter as three bfloat16 parts (8 bits of the significand each, by truncation: their sum is the float, but for bits below 2^-133, which
+// bfloat16 does not have; the parts of an infinite x are infinite, NaN and NaN: mended() in q4_kernels.h), integers as they are.
 #pragma once
 #include "internal.h"
 #include "lowbits.h"

@@ -117,3 +117,24 @@ def test_nan_through_the_activation(F, m, xt):  # noqa: F811
         for yt in FLOATS:
             got = F.linear_q4(h, x, bias=bias, x_scale=xs, out_dtype=yt, **act)
             assert same(got, y.to(yt)) and not bool(torch.signbit(got[got == 0]).any())
+
+
+@pytest.mark.parametrize("m", [1, 5, 8, 16, 40, 300])
+def test_the_smallest(F, m):  # noqa: F811
+    """16-bit x is exact down to its smallest number.  fp32 x enters with what bfloat16 holds of it, steps of 2^-133 and up: a term is off by less than that times
+    the weight's magnitude, scale (code + zero), whatever else rounds (n roundings of the sum, as for ordinary values)."""
+    g = rng(m)
+    c, k = 300, 90
+    q, s, z = weights(g, k, c, 64, True, powers=True)
+    s = s * 2.0 ** 20
+    h = F.q4_import(packed(q), s, z, group=64, c=c)
+    w, most = dense(q, s, z, 64)
+    for xt, e in ((torch.float16, -24), (torch.bfloat16, -126), (torch.bfloat16, -133), (torch.float32, -126), (torch.float32, -133)):
+        x = (ints(g, -3, 4, m, c).double() * 2.0 ** e).to(xt)
+        assert torch.equal(F.linear_q4(h, x, out_dtype=torch.float32).double(), x.double() @ w.t())
+    for e in (-100, -115, -125, -140):
+        x = torch.randn(m, c, generator=g, device="cuda") * 2.0 ** e
+        want = x.double() @ w.t()
+        got = F.linear_q4(h, x).double()
+        bound = 2.0 ** -133 * most.sum(1) + 2 * (c + 8) * 2.0 ** -24 * (x.double().abs() @ most.t())
+        assert bool(((got - want).abs() <= bound).all())
