@@ -4,15 +4,15 @@
 // 16 rows of weights, whose codes go straight from memory into the matrix cores' operands (16 bytes a lane hold 16 rows x 128 columns), as do
 // the rows of x or, in staged_kernel, from LDS.  The waves divide the blocks of 128 columns, each keeps fp32 sums of its own, which are
 // added at the end through LDS.  What bounds them: a launch and two trips to memory where the weights are few (4096 x 4096, one row of bf16: 3.7 us,
-// 2.3 TB/s), else vector instructions and the codes' way (25088 x 4096, one row of fp32: 13.3 us, 4.0 TB/s).
+// 2.3 TB/s), else vector instructions and the codes' way (25088 x 4096, one row of fp32: 13.6 us, 3.9 TB/s).
 //
 // tile_kernel (many rows of x): WN waves, a set, own 32 MT rows of x and 32 WN rows of weights.  A block of 128 columns of the rows of x is in LDS
 // while the next one is on its way there (16 bytes a lane, without registers where x is aligned); codes come from memory into registers a
 // block ahead.  WK sets may divide the blocks; their sums are added through LDS.  What a wave does per block (16 bits, MT = 4): 32 products of
 // 32 x 32 x 16, 1024 clocks of the matrix core, 19 vector instructions for every 8 codes a lane, 152, and 64 multiply-adds, since a
 // group's sum is multiplied by its scale in fp32; with addresses and staging 263.  So what counts is how few of the latter there are for a
-// product: hence 128 rows of x per decoded weight.  4096 rows of 4096 x 12288, bf16: 415 us, 0.99 PFLOP/s.  Matrix cores are busy 47 % of the
-// clocks there; decoding takes 13 %, scales 7, the rows' way to LDS 11, stores 10, LDS reads 4.  Decoding for twice the rows at once, codes
+// product: hence 128 rows of x per decoded weight.  4096 rows of 4096 x 12288, bf16: 416 us, 0.99 PFLOP/s.  Matrix cores are busy 47 % of the
+// clocks there, vector instructions as long again; decoding takes 13 %, scales 7, the rows' way to LDS 11, stores 10, LDS reads 4.  Decoding for twice the rows at once, codes
 // two blocks ahead, products and vector instructions interleaved by hand, and one barrier a block with the next block's first
 // operands read beside the last products brought 1 % or less, or lost.
 #pragma once

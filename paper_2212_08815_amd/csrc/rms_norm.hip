@@ -5,8 +5,9 @@
 // element in 16 bits), and memory bounds all but the smallest calls.  TH threads take a row: 8 to 64 where one vector of 16 bytes a
 // thread holds it, or a wave with two, so that no barrier is met; more threads for longer rows.  A thread holds N vectors, vector i of a row
 // at thread i mod TH, and issues all loads of its row before it uses the first.  A group of 32 to 128 columns lies in 4 to 32 adjacent
-// lanes.  Measured: 16384 rows of 4096 in bf16 with residual 93 us, 5.8 TB/s, in 8 bits 87; 2^19 rows of 128 91 us (with a wave a row 248);
-// one row of 4096 3.4 us, of which a launch is most.
+// lanes.  Measured: 16384 rows of 4096 in bf16 with residual 91 to 95 us, 5.7 TB/s, in 8 bits 86 to 98; 2^19 rows of 128 91 us (with a wave
+// a row 248); one row of 4096 3.2 us, of which a launch is most.  Rows past 32768 spill registers (72 to 228 bytes a thread): 512 rows of 65536 in fp32
+// 113 us, 4.7 TB/s, in bf16 79, 3.4.
 // Codes are formed in 32 bits: 2 to 7 in a million elements are so near the border between two codes that they get the other one (with
 // elementary operations in 32 bits 1 to 5).  In 64 bits none was for fp32 rows, for 10 to 25% more time; 16-bit rows have exact ties
 // that no precision settles.
