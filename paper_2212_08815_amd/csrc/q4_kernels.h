@@ -87,7 +87,12 @@ __device__ inline float mended(const Q4Args &a, bool real, int m, int k, float v
 }
 
 // The activation, which leaves NaN as it is (act_apply's ReLU gives 0 for it, as the convolutions have it)
-__device__ inline float activated(float v, int act) { return act == 1 ? (v <= 0.0f ? 0.0f : v) : act_apply(v, act); }
+__device__ inline float activated(float v, int act)
+{
+    float y = (act == 1) & (v <= 0.0f) ? 0.0f : v;
+    if (__builtin_expect((act & ~1) != 0, 0)) y = v > 0.0f ? v : v * __builtin_bit_cast(float, act);
+    return y;
+}
 
 __device__ inline void store_output(const Q4Args &a, int m, int k, float v, float bias)
 {
