@@ -487,7 +487,7 @@ fscnn_status_t fscnn_q4_destroy(fscnn_q4_t *q);
  * each group of the weights (ceil(C/group)); a group's sum is exact in 32-bit integers.
  * An x that is not finite meets every weight of its row, zeros among them (0 times infinity is NaN); other rows are not touched by it.  A sum that
  * leaves 32 bits on its way is formed again in 64: infinities and the largest values give what the definition does, whatever M is; a row of
- * such outputs takes about half a millisecond.  M == 0 is no work (pointers
+ * such outputs takes 0.1 to 0.3 ms.  M == 0 is no work (pointers
  * to x and y may be NULL then).  y must not overlap x.  workspace_dev: scratch of fscnn_linear_q4_workspace() bytes, 4-byte aligned, that belongs
  * to this call until it has run (and to a graph that captured it, as x and y do): the columns are then divided over work-groups, whose
  * sums lie there; NULL or less is right too, with sums in another order, and slower.  Allocates nothing, does not synchronise; results are

@@ -44,8 +44,8 @@ __device__ inline bool finite(float v) { return fabsf(v) < __builtin_inff(); }
 
 // The sum of an output from the definition, entry by entry, in 64 bits, where no product or sum is too large: a row of x, its scales, and codes
 // and scales from the weight row's first on.  By a whole wave: four columns a lane, the lanes' sums added in a fixed order.  (No more than
-// four, and not inlined: the kernels' own registers are what counts.)
-__device__ __attribute__((noinline)) float sum_again(const char *row, int x_type, const float *x_scale, int x_cols, const uint32_t *codes, const uint32_t *scales, int C, int group)
+// four, and in functions that are not inlined and call no others: the kernels' own registers are what counts, and none uses a stack.)
+__device__ __attribute__((always_inline)) inline float sum_again(const char *row, int x_type, const float *x_scale, int x_cols, const uint32_t *codes, const uint32_t *scales, int C, int group)
 {
     double sum = 0.0;
 #pragma unroll 1
@@ -63,22 +63,48 @@ __device__ __attribute__((noinline)) float sum_again(const char *row, int x_type
 #pragma unroll
         for (int j = 0; j < 4; ++j)
             if (c + j < C) sum += x[j] * xs * (((int)(word >> code_bit(j) & 15) - (int)(sz & 15)) * s);
+        if (__any(sum != sum)) break;        // NaN stays
     }
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
     return (float)sum;
 }
 
+__device__ __attribute__((noinline)) float one_again(const char *row, int x_type, const float *x_scale, int x_cols, const uint32_t *codes, const uint32_t *scales, int C, int group)
+{
+    return sum_again(row, x_type, x_scale, x_cols, codes, scales, C, group);
+}
+
+// Whether a row of x holds a NaN; by a whole wave
+__device__ __attribute__((always_inline)) inline int has_nan(const char *row, int x_type, int C)
+{
+    int nan = 0;
+#pragma unroll 1
+    for (int c = threadIdx.x & 63; !__any(nan) && c - (int)(threadIdx.x & 63) < C; c += 256)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float x = load_float(row, c + 64 * j < C ? c + 64 * j : C - 1, x_type);
+            nan |= x != x;
+        }
+    return __any(nan);
+}
+
+__device__ __attribute__((noinline)) int nan_in_row(const char *row, int x_type, int C) { return has_nan(row, x_type, C); }
+
 // v of the wave's lanes, each the sum of output (m, k) if it is one (`real`): those that are not finite are made again.  A kernel's may be that
 // where the definition's is finite (codes times x, or a group's sum before it meets its scale, past the largest float), or NaN where it is
-// infinite (an infinite x in three parts, or less the zero point's share).  bf16, 4096 columns: 64 x 4096 outputs 16 us, 0.5 ms if those of one row are
-// made again; 4096 x 12288 415 us, 430 ms if all are.  Looking for them costs up to 2 % (0.1 us of the smallest calls).
+// infinite (an infinite x in three parts, or less the zero point's share).  bf16, 4096 columns: 64 x 4096 outputs 16 us, 0.15 ms if those of one row are
+// made again; 4096 x 12288 415 us, 160 ms if all are, 0.9 if all are NaN.  Looking for them costs up to 2 % (0.1 us of the smallest calls).
 __device__ inline float mended(const Q4Args &a, bool real, int m, int k, float v)
 {
+    int looked = -1, nan = 0;                 // the row of x that was looked at last, for a NaN: its sums are NaN as they are
     for (unsigned long long todo = __ballot(real && !finite(v)); __builtin_expect(todo != 0, 0); todo &= todo - 1) {
         const int lane = __builtin_ctzll(todo), mm = __builtin_amdgcn_readlane(m, lane), kk = __builtin_amdgcn_readlane(k, lane);
+        if (mm != looked && a.x_type != FSCNN_I8) nan = nan_in_row(a.x + mm * a.ldx, a.x_type, a.C);
+        looked = mm;
+        if (nan) continue;
         const long long tile = kk >> 4;
-        const float s = sum_again(a.x + mm * a.ldx, a.x_type, a.x_scale ? a.x_scale + (long long)mm * a.x_cols : nullptr, a.x_cols,
+        const float s = one_again(a.x + mm * a.ldx, a.x_type, a.x_scale ? a.x_scale + (long long)mm * a.x_cols : nullptr, a.x_cols,
                                   reinterpret_cast<const uint32_t *>(a.codes) + (tile * a.blocks * 256 + (kk & 15) * 4),
                                   a.scales + (tile * a.blocks * (64 >> (a.steps >> 1)) + (kk & 15)), a.C, a.steps * 32);
         if ((int)(threadIdx.x & 63) == lane) v = s;
@@ -92,6 +118,23 @@ __device__ inline float activated(float v, int act)
     float y = (act == 1) & (v <= 0.0f) ? 0.0f : v;
     if (__builtin_expect((act & ~1) != 0, 0)) y = v > 0.0f ? v : v * __builtin_bit_cast(float, act);
     return y;
+}
+
+// Lane l's output l % 32 of a row of x and 32 weight rows (codes, scales: of the first one on, which is a tile's first), of those that `bad` has a bit for, by a wave.
+// NaN where the row of x holds one.
+__device__ __attribute__((noinline)) float row_again(uint32_t bad, const char *row, int x_type, const float *x_scale, int x_cols, const uint32_t *codes, const uint32_t *scales,
+                                                     int blocks, int C, int group)
+{
+    float v = __builtin_nanf("");
+    if (x_type != FSCNN_I8 && has_nan(row, x_type, C)) bad = 0;
+#pragma unroll 1
+    for (bad = __builtin_amdgcn_readfirstlane(bad); bad; bad &= bad - 1) {
+        const int at = __builtin_ctz(bad);
+        const long long tile = (at >> 4) * (long long)blocks;
+        const float s = sum_again(row, x_type, x_scale, x_cols, codes + (tile * 256 + (at & 15) * 4), scales + (tile * (128 / group) * 16 + (at & 15)), C, group);
+        if ((int)(threadIdx.x & 31) == at) v = s;
+    }
+    return v;
 }
 
 __device__ inline void store_output(const Q4Args &a, int m, int k, float v, float bias)
@@ -365,13 +408,12 @@ __global__ void __launch_bounds__(WN * WK * 64, XT == FSCNN_F32 ? 1 : 2) tile_ke
     constexpr int kSums = (WK - 1) * kSet * MT * 4;  // in 16 bytes, at the end
     constexpr int kChunksOfSet = 2 * kBuf + kScales;
     static_assert(kPer * kSet == kRows * kCh, "a whole number of chunks a thread");
-    static_assert(kRows <= kSet * WK && (!GS || kRows <= kSet), "a thread a row");
-    static_assert(1024 * WN % (kSet * WK) == 0, "outputs in whole turns");
+    static_assert(!GS || kRows <= kSet, "a thread a row");
     constexpr int kPitch = 32 * WN + 8, kArea = 32 * kPitch;   // of outputs, in floats: rows 4 apart half of the banks apart
     constexpr int kNeed = kSums * 4 > 2 * kArea ? kSums : (2 * kArea + 3) / 4;
     __shared__ u4v lds[kChunksOfSet * WK > kNeed ? kChunksOfSet * WK : kNeed];
-    __shared__ int odd[MT];                   // rows of 32 whose sums are looked at again
-    if (threadIdx.x < MT) odd[threadIdx.x] = 0;   // (there is a barrier before they are read or set)
+    __shared__ int odd;                       // some sums are not finite
+    if (threadIdx.x == 0) odd = 0;            // (there is a barrier before it is read or set)
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wk = wave / WN, in_set = wave % WN, half = lane >> 5;
     // panels of 8 tiles of x: work-groups that run together share both operands
@@ -604,19 +646,19 @@ __global__ void __launch_bounds__(WN * WK * 64, XT == FSCNN_F32 ? 1 : 2) tile_ke
         if (wk == 0)
 #pragma unroll
             for (int i = 0; i < 16; ++i) all[i & 3] += fabsf(total[u][i]);
-        if (!finite(all[0] + all[1] + (all[2] + all[3]))) odd[u] = 1;   // one of them is not, or (no harm) their sum alone
+        if (!finite(all[0] + all[1] + (all[2] + all[3]))) odd = 1;   // one of them is not, or (no harm) their sum alone
         if (wk == 0)
 #pragma unroll
             for (int i = 0; i < 16; ++i) area[(u & 1) * kArea + (8 * (i >> 2) + 4 * half + (i & 3)) * kPitch + in_set * 32 + (lane & 31)] = total[u][i];
     };
-    const auto store = [&](int u, bool again, auto type) {
+    const auto store = [&](int u, auto type) {
         using E = typename Elem<decltype(type)::value>::type;
         constexpr int kV = 16 / (int)sizeof(E), kRow = 32 * WN / kV;   // outputs of a thread; threads of a row
         for (int at = threadIdx.x; at < 32 * kRow; at += kSet * WK) {
             const int r = at / kRow, c = at % kRow * kV, m = m0 + u * 32 + r, k = cols0 + c;
             if (m >= a.M || k >= a.K) continue;
             const float *f = area + (u & 1) * kArea + r * kPitch + c;
-            const float xs = kInt && !GS && !again ? a.x_scale[m] : 1.0f;
+            const float xs = kInt && !GS ? a.x_scale[m] : 1.0f;
             E e[kV];
 #pragma unroll
             for (int j = 0; j < kV; ++j) {
@@ -632,26 +674,41 @@ __global__ void __launch_bounds__(WN * WK * 64, XT == FSCNN_F32 ? 1 : 2) tile_ke
                     if (k + j < a.K) y[j] = e[j];
         }
     };
-    const auto look = [&](int u) {            // (with the rows' scales; a whole number of turns for every wave)
-#pragma unroll 1
-        for (int at = threadIdx.x; at < 1024 * WN; at += kSet * WK) {
-            const int r = at / (32 * WN), m = m0 + u * 32 + r, k = cols0 + at % (32 * WN);
-            float *f = area + (u & 1) * kArea + r * kPitch + at % (32 * WN);
-            const bool real = m < a.M && k < a.K;
-            *f = mended(a, real, m, k, kInt && !GS && real ? *f * a.x_scale[m] : *f);
-        }
-        __syncthreads();
-    };
     __syncthreads();
 #pragma unroll
     for (int u = 0; u < MT; ++u) {            // (two areas: a barrier each)
         put(u);
         __syncthreads();
-        const bool again = odd[u] != 0;       // (the same for all: written before the barrier only)
-        if (__builtin_expect(again, 0)) look(u);
-        if (a.y_type == FSCNN_F32) store(u, again, std::integral_constant<int, FSCNN_F32>{});
-        else if (a.y_type == FSCNN_F16) store(u, again, std::integral_constant<int, FSCNN_F16>{});
-        else store(u, again, std::integral_constant<int, FSCNN_BF16>{});
+        if (a.y_type == FSCNN_F32) store(u, std::integral_constant<int, FSCNN_F32>{});
+        else if (a.y_type == FSCNN_F16) store(u, std::integral_constant<int, FSCNN_F16>{});
+        else store(u, std::integral_constant<int, FSCNN_BF16>{});
+    }
+    if (__builtin_expect(odd != 0, 0)) {      // (the same for all: written before the last barrier)
+        __syncthreads();                      // what has been stored is in its place
+        if (wk > 0) return;
+        const int k = n0 + (lane & 31);
+        unsigned long long bad = 0;           // which of the lane's
+#pragma unroll
+        for (int u = 0; u < MT; ++u)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) bad |= (unsigned long long)!finite(total[u][i]) << (u * 16 + i);
+#pragma unroll 1
+        for (int e = 0; e < MT * 16; ++e) {
+            const int m = m0 + (e >> 4) * 32 + 8 * ((e & 15) >> 2) + (e & 3), mine = m + 4 * half;
+            bool again = bad >> e & 1;
+            if (kInt && !GS && mine < a.M) again |= !finite(a.x_scale[mine]);
+            const unsigned long long lanes = __ballot(again && mine < a.M && k < a.K);
+#pragma unroll 1
+            for (int h = 0; h < 2; ++h) {
+                const uint32_t of_row = (uint32_t)(lanes >> (32 * h));
+                if (!of_row) continue;
+                const int r = m + 4 * h;
+                const long long tile = n0 >> 4;
+                const float v = row_again(of_row, a.x + r * a.ldx, XT, kInt ? a.x_scale + (long long)r * a.x_cols : nullptr, a.x_cols,
+                                          reinterpret_cast<const uint32_t *>(a.codes) + tile * a.blocks * 256, a.scales + tile * a.blocks * (kGroups * 16), a.blocks, a.C, 32 * STEPS);
+                if (half == h && (of_row >> (lane & 31) & 1)) store_output(a, r, k, v, a.bias ? a.bias[k] : 0.0f);
+            }
+        }
     }
 }
 

@@ -138,3 +138,25 @@ def test_the_smallest(F, m):  # noqa: F811
         got = F.linear_q4(h, x).double()
         bound = 2.0 ** -133 * most.sum(1) + 2 * (c + 8) * 2.0 ** -24 * (x.double().abs() @ most.t())
         assert bool(((got - want).abs() <= bound).all())
+
+
+@pytest.mark.parametrize("xt", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("m,c,k", SIZES)
+def test_nan_beside_infinities_and_the_largest(F, m, c, k, xt):  # noqa: F811
+    """A NaN anywhere in a row of x makes all of its outputs NaN, whatever else the row holds; rows around it are the definition's."""
+    case = SIZES.index((m, c, k))
+    g = rng(case)
+    q, s, z = weights(g, k, c, 64, True, powers=True)
+    s = s * 2.0 ** -20
+    h = F.q4_import(packed(q), s, z, group=64, c=c)
+    w = dense(q, s, z, 64)[0]
+    x = (ints(g, -3, 4, m, c).float() * 2.0 ** 126).to(xt)
+    want = x.double() @ w.t()
+    for row, col in ((0, c - 1), (m // 2, 0), (m - 1, c // 2)):
+        x[row, col] = float("nan")
+        want[row] = float("nan")
+    x[0, 0] = INF
+    x[m - 1, 1] = -INF
+    for a in (x, apart(x, 3, 1)):
+        assert same(F.linear_q4(h, a, out_dtype=torch.float32), want.float())
+        assert same(F.linear_q4(h, a, relu=True), want.clamp(min=0).to(xt))
