@@ -208,8 +208,8 @@ namespace fscnn {
 // ---- q4.hip: 4-bit weights.  Word s of lane l of a block holds the eight codes of row l % 16 whose columns in the block are
 // 32 s + 8 (l / 16) + j, j = 0..7: code j in nibble 2 j for j < 4, else in nibble 2 (j - 4) + 1.  (A step of 32 columns of the matrix
 // cores' 16-row operand; the nibbles of a parity, masked out, are four codes in bytes.)  Codes of columns past C may be any, the
-// kernels read x as zero there; rows past K and groups past C have a scale of zero.  A scale is the word of its value as a float, which 16-bit types leave at least 13 low bits of: the zero
-// point is in the low four.
+// kernels read x as zero there; rows past K and groups past C have a scale of zero.  A scale is the word of its value
+// as a float, which 16-bit types leave at least 13 low bits of: the zero point is in the low four.
 constexpr int kQ4Block = 128;
 __host__ __device__ inline int code_bit(int j) { return j < 4 ? 8 * j : 8 * (j - 4) + 4; }   // first bit of column j's code in its word
 inline long long q4_tiles(int K) { return ((long long)K + 15) / 16; }

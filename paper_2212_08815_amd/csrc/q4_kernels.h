@@ -12,8 +12,8 @@
 // 32 x 32 x 16, 1024 clocks of the matrix core, 19 vector instructions for every 8 codes a lane, 152, and 64 multiply-adds, since a
 // group's sum is multiplied by its scale in fp32; with addresses and staging 263.  So what counts is how few of the latter there are for a
 // product: hence 128 rows of x per decoded weight.  4096 rows of 4096 x 12288, bf16: 416 us, 0.99 PFLOP/s.  Matrix cores are busy 47 % of the
-// clocks there, vector instructions as long again; decoding takes 13 %, scales 7, the rows' way to LDS 11, stores 10, LDS reads 4.  Decoding for twice the rows at once, codes
-// two blocks ahead, products and vector instructions interleaved by hand, and one barrier a block with the next block's first
+// clocks there, vector instructions as long again; decoding takes 13 %, scales 7, the rows' way to LDS 11, stores 10, LDS reads 4.
+// Decoding for twice the rows at once, codes two blocks ahead, products and vector instructions interleaved by hand, and one barrier a block with the next block's first
 // operands read beside the last products brought 1 % or less, or lost.
 #pragma once
 #include <type_traits>
@@ -45,7 +45,8 @@ __device__ inline bool finite(float v) { return fabsf(v) < __builtin_inff(); }
 // The sum of an output from the definition, entry by entry, in 64 bits, where no product or sum is too large: a row of x, its scales, and codes
 // and scales from the weight row's first on.  By a whole wave: four columns a lane, the lanes' sums added in a fixed order.  (No more than
 // four, and in functions that are not inlined and call no others: the kernels' own registers are what counts, and none uses a stack.)
-__device__ __attribute__((always_inline)) inline float sum_again(const char *row, int x_type, const float *x_scale, int x_cols, const uint32_t *codes, const uint32_t *scales, int C, int group)
+__device__ __attribute__((always_inline)) inline float sum_again(const char *row, int x_type, const float *x_scale, int x_cols, const uint32_t *codes,
+                                                                  const uint32_t *scales, int C, int group)
 {
     double sum = 0.0;
 #pragma unroll 1
@@ -70,7 +71,8 @@ __device__ __attribute__((always_inline)) inline float sum_again(const char *row
     return (float)sum;
 }
 
-__device__ __attribute__((noinline)) float one_again(const char *row, int x_type, const float *x_scale, int x_cols, const uint32_t *codes, const uint32_t *scales, int C, int group)
+__device__ __attribute__((noinline)) float one_again(const char *row, int x_type, const float *x_scale, int x_cols, const uint32_t *codes,
+                                                           const uint32_t *scales, int C, int group)
 {
     return sum_again(row, x_type, x_scale, x_cols, codes, scales, C, group);
 }
@@ -120,10 +122,10 @@ __device__ inline float activated(float v, int act)
     return y;
 }
 
-// Lane l's output l % 32 of a row of x and 32 weight rows (codes, scales: of the first one on, which is a tile's first), of those that `bad` has a bit for, by a wave.
-// NaN where the row of x holds one.
-__device__ __attribute__((noinline)) float row_again(uint32_t bad, const char *row, int x_type, const float *x_scale, int x_cols, const uint32_t *codes, const uint32_t *scales,
-                                                     int blocks, int C, int group)
+// Lane l's output l % 32 of a row of x and 32 weight rows (codes, scales: of the first one on, which is a tile's first), of those that `bad` has a bit
+// for, by a wave.  NaN where the row of x holds one.
+__device__ __attribute__((noinline)) float row_again(uint32_t bad, const char *row, int x_type, const float *x_scale, int x_cols, const uint32_t *codes,
+                                                     const uint32_t *scales, int blocks, int C, int group)
 {
     float v = __builtin_nanf("");
     if (x_type != FSCNN_I8 && has_nan(row, x_type, C)) bad = 0;
@@ -705,7 +707,8 @@ __global__ void __launch_bounds__(WN * WK * 64, XT == FSCNN_F32 ? 1 : 2) tile_ke
                 const int r = m + 4 * h;
                 const long long tile = n0 >> 4;
                 const float v = row_again(of_row, a.x + r * a.ldx, XT, kInt ? a.x_scale + (long long)r * a.x_cols : nullptr, a.x_cols,
-                                          reinterpret_cast<const uint32_t *>(a.codes) + tile * a.blocks * 256, a.scales + tile * a.blocks * (kGroups * 16), a.blocks, a.C, 32 * STEPS);
+                                          reinterpret_cast<const uint32_t *>(a.codes) + tile * a.blocks * 256, a.scales + tile * a.blocks * (kGroups * 16),
+                                          a.blocks, a.C, 32 * STEPS);
                 if (half == h && (of_row >> (lane & 31) & 1)) store_output(a, r, k, v, a.bias ? a.bias[k] : 0.0f);
             }
         }
